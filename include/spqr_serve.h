@@ -50,7 +50,7 @@ typedef struct spqr_step_t {
   int32_t max_pages;             /* columns of table, >= 1                                                            */
   int32_t mask_words;            /* 64-bit words of a row's mask, 1 .. 4; 0: no masks, new tokens see those before them */
   int32_t dtype;                 /* SPQR_F16 or SPQR_BF16: k, v, and q and out of the attention                        */
-  int32_t heads, kv_heads;       /* query heads, a multiple of kv_heads; head h reads kv head h / (heads / kv_heads)  */
+  int32_t heads, kv_heads;       /* query heads, a multiple of kv_heads, <= 1024; h reads kv head h / (heads / kv_heads) */
   int32_t head_dim;              /* 64, 96, 128 or 256                                                                */
   int32_t page;                  /* rows of a page: 16, 32, 64, 128 or 256                                            */
   int32_t pages, layers;         /* pages * page < 2^31                                                               */

@@ -19,6 +19,7 @@
 #ifndef SPQR_ATTENTION_INTERNAL_H_
 #define SPQR_ATTENTION_INTERNAL_H_
 #include <cmath>
+#include <type_traits>
 
 #include "spqr_serve.h"
 
@@ -33,6 +34,9 @@ struct Attend {
   float *part_o, *part_ml;       // [2 * workgroups][rows of a chunk][D], [...][2]: reference, sum
   int requests, tokens, group, kv_heads, log_page, pages, max_pages, words;
   float scale2;                  // scale * log2(e)
+  float inv_group;
+  int workgroups;
+  double inv_workgroups;
 };
 
 struct AttendPlan {              // of a launch; host
@@ -106,6 +110,7 @@ __device__ __forceinline__ Request request_of(const Attend& a, int r, int chunk_
 __device__ __forceinline__ int64_t scan_requests(const Attend& a, int chunk_rows, int64_t* ends, int64_t* wave_sums) {
   const int tid = threadIdx.x, lane = tid & 63, each = (a.requests + 255) / 256;
   int64_t sum = 0;
+#pragma unroll 1
   for (int i = 0; i < each; ++i) {
     const int r = tid * each + i;
     if (r < a.requests) sum += request_of(a, r, chunk_rows).work(a.kv_heads), ends[r] = sum;
@@ -122,14 +127,37 @@ __device__ __forceinline__ int64_t scan_requests(const Attend& a, int chunk_rows
     if (w < tid >> 6) before += wave_sums[w];
     all += wave_sums[w];
   }
+#pragma unroll 1
   for (int i = 0; i < each; ++i)
     if (tid * each + i < a.requests) ends[tid * each + i] += before;
   __syncthreads();
   return all;
 }
 
-__device__ __forceinline__ int64_t part_size(int64_t work, int workgroups) {
-  return max((int64_t)kLeast, (work + workgroups - 1) / workgroups);
+// Tiles of a workgroup's part: enough for all parts together.
+__device__ __forceinline__ int64_t part_size(const Attend& a, int64_t work) {
+  int64_t q = (int64_t)((double)work * a.inv_workgroups);
+  if (q * a.workgroups < work) ++q;
+  return max((int64_t)kLeast, q);
+}
+
+// x / tiles, x < tiles * 2^24: by the reciprocal, put right.
+__device__ __forceinline__ int which_pair(int64_t x, int tiles) {
+  int q = (int)((double)x * __builtin_amdgcn_rcp((double)tiles));
+  if ((int64_t)q * tiles > x) --q;
+  if ((int64_t)(q + 1) * tiles <= x) ++q;
+  return q;
+}
+
+// row / group for rows of a request, group <= 1024: the quotient is at most 256 and off by less than 2^-14 before it is cut.
+__device__ __forceinline__ int token_of(const Attend& a, int row) { return (int)(((float)row + 0.5f) * a.inv_group); }
+
+// Parts that start at or before tile x.
+__device__ __forceinline__ int64_t parts_to(int64_t x, int64_t part) {
+  int64_t q = (int64_t)((double)x * __builtin_amdgcn_rcp((double)part));
+  if (q * part > x) --q;
+  if ((q + 1) * part <= x) ++q;
+  return q + 1;
 }
 
 // The request that has tile x of the line, x < ends[requests - 1].
@@ -162,7 +190,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), x16 = lane & 15, g = lane >> 4;
   const int64_t work = scan_requests(a, kRows, ends, wave_sums);
-  const int64_t part = part_size(work, gridDim.x);
+  const int64_t part = part_size(a, work);
   const int64_t begin = blockIdx.x * part, end = min(work, begin + part);
   if (begin >= end) return;
   int r = find_request(ends, a.requests, begin);
@@ -174,7 +202,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     r = uniform(r);
     const Request rq = request_of(a, r, kRows);
     const int64_t in_request = at - (r == 0 ? 0 : ends[r - 1]);
-    const int pair = uniform((int)(in_request / rq.tiles));
+    const int pair = uniform(which_pair(in_request, rq.tiles));
     const int t0 = uniform((int)(in_request - (int64_t)pair * rq.tiles));
     const int t1 = uniform((int)min((int64_t)rq.tiles, t0 + (end - at)));
     const int h = pair / rq.chunks, chunk = pair - h * rq.chunks;
@@ -190,7 +218,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     for (int m = 0; m < MT; ++m) {
       const int row = row0 + 16 * m + x16;
       const bool live = row < rq.rows * a.group;
-      token[m] = live ? row / a.group : -1;
+      token[m] = live ? token_of(a, row) : -1;
       const T* from = static_cast<const T*>(a.q) + (int64_t)(rq.first_row + token[m]) * a.q_stride + (h * a.group + row - token[m] * a.group) * D + 8 * g;
 #pragma unroll
       for (int c = 0; c < DC; ++c) q[m][c] = live ? *reinterpret_cast<const u32x4*>(from + 32 * c) : u32x4{0, 0, 0, 0};
@@ -205,48 +233,44 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       for (int n = 0; n < E; ++n) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // page ids of a tile's two halves; one that is not there is page 0, of which nothing is seen
+    // page ids of a tile's two halves
     auto page_ids = [&](int t, int& id0, int& id1) {
-      const int p0 = (t * kTile) >> a.log_page, p1 = (t * kTile + 16) >> a.log_page;
-      id0 = p0 < a.max_pages ? table[p0] : -1;
-      id1 = p1 < a.max_pages ? table[p1] : -1;
+      id0 = table[min((t * kTile) >> a.log_page, a.max_pages - 1)];
+      id1 = table[min((t * kTile + 16) >> a.log_page, a.max_pages - 1)];
     };
-    auto half_offset = [&](int id, int key) { return (int64_t)((unsigned)id < (unsigned)a.pages ? id : 0) * page_elements + (key & (page - 1)) * D; };
+    auto there = [&](int id) { return (unsigned)id < (unsigned)a.pages; };
+    // one that is not there is page 0, of which nothing is seen
+    auto half_offset = [&](int id, int key) { return (int64_t)(there(id) ? id : 0) * page_elements + (key & (page - 1)) * D; };
 
+    const uint32_t k_lane = x16 * D + 8 * g, v_lane = 4 * g * D + E * x16;
     u32x4 kf[2][DC];
     uint32_t vf[8][EW];
-    int id0, id1, next0 = -1, next1 = -1;
-    auto load_keys = [&](int t, int i0, int i1) {
+    int id0, id1, next0, next1;
+    auto load_keys = [&](int t, int i0, int i1, uint32_t k_lane) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const T* base = kh + half_offset(u ? i1 : i0, t * kTile + 16 * u);
 #pragma unroll
-        for (int c = 0; c < DC; ++c) kf[u][c] = *reinterpret_cast<const u32x4*>(base + x16 * D + 8 * g + 32 * c);
+        for (int c = 0; c < DC; ++c) kf[u][c] = *reinterpret_cast<const u32x4*>(base + (k_lane + 32 * c));
       }
     };
-    auto load_values = [&](int t, int i0, int i1) {
+    auto load_values = [&](int t, int i0, int i1, uint32_t v_lane) {
 #pragma unroll
       for (int u = 0; u < 2; ++u) {
         const T* base = vh + half_offset(u ? i1 : i0, t * kTile + 16 * u);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          __builtin_memcpy(vf[4 * u + i], __builtin_assume_aligned(base + (4 * g + i) * D + E * x16, E % 8 == 0 ? 16 : E % 4 == 0 ? 8 : 4), 4 * EW);
+          __builtin_memcpy(vf[4 * u + i], __builtin_assume_aligned(base + (v_lane + i * D), E % 8 == 0 ? 16 : E % 4 == 0 ? 8 : 4), 4 * EW);
       }
     };
 
-    int t = t0 + wave;
-    if (t < t1) {
-      page_ids(t, id0, id1);
-      load_keys(t, id0, id1);
-      load_values(t, id0, id1);
-      if (t + 4 < t1) page_ids(t + 4, next0, next1);
-    }
-    for (; t < t1; t += 4) {
-      const bool more = t + 4 < t1;
-      f32x4 s[MT][2];
+    // the steps of a tile
+    f32x4 s[MT][2];
+    uint32_t p[MT][4], seen[MT];
+    auto scores = [&] {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        if (16 * m >= live_rows) continue;
+        if (m > 0 && 16 * m >= live_rows) continue;
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           s[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -254,14 +278,94 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
           for (int c = 0; c < DC; ++c) s[m][u] = Matrix<T>::product(kf[u][c], q[m][c], s[m][u]);
         }
       }
-      if (more) load_keys(t + 4, next0, next1);
+    };
+    auto probabilities = [&](auto masked_tile) {
+      constexpr bool masked = decltype(masked_tile)::value;
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if (m > 0 && 16 * m >= live_rows) continue;
+        float z[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = s[m][j >> 2][j & 3] * a.scale2;
+        if constexpr (masked) {
+#pragma unroll
+          for (int j = 0; j < 8; ++j) z[j] = seen[m] >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1 ? z[j] : -INFINITY;
+        }
+        float most = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
+        if (__any(most > top[m] + 8.f)) {
+          most = fmaxf(most, __shfl_xor(most, 16));
+          most = fmaxf(most, __shfl_xor(most, 32));
+          const float now = most > top[m] + 8.f ? most : top[m];
+          const float back = now == top[m] ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
+          top[m] = now;
+          sum[m] *= back;
+#pragma unroll
+          for (int n = 0; n < E; ++n) o[m][n] *= back;
+        }
+        const float ref = top[m] == -INFINITY ? 0.f : top[m];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = __builtin_amdgcn_exp2f(z[j] - ref);
+        sum[m] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) p[m][j] = pack<T>(z[2 * j], z[2 * j + 1]);
+      }
 
-      // keys that some row may not see
-      const bool there0 = (unsigned)id0 < (unsigned)a.pages, there1 = (unsigned)id1 < (unsigned)a.pages;
+    };
+    u32x4 vt[E];
+    auto transpose = [&] {
+#pragma unroll
+      for (int n = 0; n < E; ++n)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) vt[n][j] = __builtin_amdgcn_perm(vf[2 * j + 1][n / 2], vf[2 * j][n / 2], n & 1 ? 0x07060302 : 0x05040100);
+    };
+    auto outputs = [&] {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        if (m > 0 && 16 * m >= live_rows) continue;
+        const u32x4 b = {p[m][0], p[m][1], p[m][2], p[m][3]};
+#pragma unroll
+        for (int n = 0; n < E; ++n) o[m][n] = Matrix<T>::product(vt[n], b, o[m][n]);
+      }
+    };
+
+    // Tiles of cached keys that are all there.  The next tile's loads go into the registers that this one's products have read;
+    // behind the last tile they are made all the same, without a branch (behind which the compiler would wait), but of one
+    // line.
+    const int plain_end = min(t1, min(rq.cached, rq.keys) / kTile);
+    int t = t0 + wave;
+    if (t < plain_end) {
+      page_ids(t, id0, id1);
+      load_keys(t, id0, id1, k_lane);
+      load_values(t, id0, id1, v_lane);
+      int following = min(t + 4, plain_end - 1);
+      page_ids(following, next0, next1);
+      while (there(id0) && there(id1)) {
+        const bool more = t + 4 < plain_end;
+        scores();
+        __builtin_amdgcn_sched_barrier(0);
+        load_keys(following, next0, next1, more ? k_lane : 0);
+        probabilities(std::false_type());
+        transpose();
+        __builtin_amdgcn_sched_barrier(0);
+        load_values(following, next0, next1, more ? v_lane : 0);
+        outputs();
+        t += 4;
+        if (!more) break;
+        id0 = next0;
+        id1 = next1;
+        following = min(t + 4, plain_end - 1);
+        page_ids(following, next0, next1);
+      }
+    }
+    // the last cached keys, the new ones, and what lies on and behind pages that are not there
+    for (; t < t1; t += 4) {
+      page_ids(t, id0, id1);
+      load_keys(t, id0, id1, k_lane);
+      load_values(t, id0, id1, v_lane);
       const int key0 = t * kTile;
-      const bool plain = key0 + kTile <= rq.cached && key0 + kTile <= rq.keys && there0 && there1;
-      uint32_t seen[MT];
-      if (!plain) {
+      scores();
+      {
+        const bool there0 = there(id0) && key0 >> a.log_page < a.max_pages, there1 = there(id1) && (key0 + 16) >> a.log_page < a.max_pages;
         const int left = rq.keys - key0;
         uint32_t exist = left >= 32 ? ~0u : (1u << left) - 1;
         if (!there0) exist &= 0xFFFF0000u;
@@ -295,101 +399,54 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
           for (int e = 0; e < EW; ++e) vf[j][e] = on ? vf[j][e] : 0;
         }
       }
-
-      uint32_t p[MT][4];
-      float pf[MT][8];
-#pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        if (16 * m >= live_rows) continue;
-        float z[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = s[m][j >> 2][j & 3] * a.scale2;
-        if (!plain) {
-#pragma unroll
-          for (int j = 0; j < 8; ++j) z[j] = seen[m] >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1 ? z[j] : -INFINITY;
-        }
-        float most = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-        if (__any(most > top[m] + 8.f)) {
-          most = fmaxf(most, __shfl_xor(most, 16));
-          most = fmaxf(most, __shfl_xor(most, 32));
-          const float now = most > top[m] + 8.f ? most : top[m];
-          const float back = now == top[m] ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
-          top[m] = now;
-          sum[m] *= back;
-#pragma unroll
-          for (int n = 0; n < E; ++n) o[m][n] *= back;
-        }
-        const float ref = top[m] == -INFINITY ? 0.f : top[m];
-        float part_sum = 0.f;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          pf[m][j] = __builtin_amdgcn_exp2f(z[j] - ref);
-          part_sum += pf[m][j];
-        }
-        sum[m] += part_sum;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) p[m][j] = pack<T>(pf[m][2 * j], pf[m][2 * j + 1]);
-      }
-
-      if (!plain) {
+      probabilities(std::true_type());
+      {
         // Infinities and NaN among the values: 0 * inf would reach rows that do not see the key.  Such a key is taken out of
-        // the matrix product and added by the rows that see it.
-        bool bad[8], any = false;
+        // the matrix product and added by the rows that see it; the probabilities pass through this wavefront's part of `so`.
+        uint32_t bad = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          bad[j] = false;
+          bool mine = false;
 #pragma unroll
           for (int e = 0; e < EW; ++e)
-            bad[j] |= (vf[j][e] & Matrix<T>::kExponent) == Matrix<T>::kExponent || (vf[j][e] >> 16 & Matrix<T>::kExponent) == Matrix<T>::kExponent;
-          any |= bad[j];
+            mine |= (vf[j][e] & Matrix<T>::kExponent) == Matrix<T>::kExponent || (vf[j][e] >> 16 & Matrix<T>::kExponent) == Matrix<T>::kExponent;
+          const uint64_t votes = __ballot(mine);
+#pragma unroll
+          for (int k = 0; k < 4; ++k) bad |= (votes >> (16 * k) & 0xFFFF) != 0 ? 1u << (16 * (j >> 2) + 4 * k + (j & 3)) : 0;
         }
-        if (__any(any)) {
+        if (bad != 0) {
+          uint32_t* kept = reinterpret_cast<uint32_t*>(&so[wave][0][0][0]);
 #pragma unroll
-          for (int j = 0; j < 8; ++j) {
-            const uint64_t votes = __ballot(bad[j]);
+          for (int m = 0; m < MT; ++m)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) kept[(4 * m + j) * 64 + lane] = 16 * m < live_rows ? p[m][j] : 0;
+          __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
 #pragma unroll 1
-            for (int gg = 0; gg < 4; ++gg) {
-              if ((votes >> (16 * gg) & 0xFFFF) == 0) continue;
-              const int in_tile = 16 * (j >> 2) + 4 * gg + (j & 3);
-              const T* v = vh + half_offset(j < 4 ? id0 : id1, key0 + 16 * (j >> 2)) + (4 * gg + (j & 3)) * D + E * 4 * g;
+          for (uint32_t left = bad; left != 0; left &= left - 1) {
+            const int key = __builtin_ctz(left), j = 4 * (key >> 4) + (key & 3), of = key >> 2 & 3;
+            const T* v = vh + half_offset(key < 16 ? id0 : id1, key0 + (key & 16)) + (key & 15) * D + E * 4 * g;
 #pragma unroll
-              for (int m = 0; m < MT; ++m) {
-                if (16 * m >= live_rows) continue;
-                const float weight = __shfl(pf[m][j], 16 * gg + x16);
-                if (seen[m] >> in_tile & 1) {
+            for (int m = 0; m < MT; ++m) {
+              const uint32_t both = kept[(4 * m + (j >> 1)) * 64 + 16 * of + x16];
+              const float weight = (float)__builtin_bit_cast(T, (uint16_t)(j & 1 ? both >> 16 : both));
+              if (16 * m < live_rows && (seen[m] >> key & 1)) {
 #pragma unroll
-                  for (int n = 0; n < E; ++n)
+                for (int n = 0; n < E; ++n)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) o[m][n][i] += weight * (float)v[E * i + n];
-                }
-              }
-              if (g == gg) {
-#pragma unroll
-                for (int e = 0; e < EW; ++e) vf[j][e] = 0;
+                  for (int i = 0; i < 4; ++i) o[m][n][i] += weight * (float)v[E * i + n];
               }
             }
           }
+#pragma unroll
+          for (int j = 0; j < 8; ++j) {
+            const bool out = bad >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1;
+#pragma unroll
+            for (int e = 0; e < EW; ++e) vf[j][e] = out ? 0 : vf[j][e];
+          }
         }
       }
-
-#pragma unroll
-      for (int n = 0; n < E; ++n) {
-        u32x4 vt;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) vt[j] = __builtin_amdgcn_perm(vf[2 * j + 1][n / 2], vf[2 * j][n / 2], n & 1 ? 0x07060302 : 0x05040100);
-#pragma unroll
-        for (int m = 0; m < MT; ++m) {
-          if (16 * m >= live_rows) continue;
-          u32x4 b = {p[m][0], p[m][1], p[m][2], p[m][3]};
-          o[m][n] = Matrix<T>::product(vt, b, o[m][n]);
-        }
-      }
-      if (more) {
-        load_values(t + 4, next0, next1);
-        id0 = next0;
-        id1 = next1;
-        if (t + 8 < t1) page_ids(t + 8, next0, next1);
-      }
+      transpose();
+      outputs();
     }
 
     // the four wavefronts' parts, 16 rows at a time
@@ -422,7 +479,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       const int in_chunk = 16 * m + x16, d = E * (4 * g + wave);
       if (in_chunk < live_rows) {
         if (whole) {
-          const int row = row0 + in_chunk, tok = row / a.group;
+          const int row = row0 + in_chunk, tok = token_of(a, row);
           const float c = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
           for (int n = 0; n < E; ++n) y[n] = all == 0.f ? 0.f : y[n] * c;
@@ -447,24 +504,25 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
 // them than parts, else the one that the x-th cut divides, if it is its first cut; y: rows.  A quarter of a wavefront (or less)
 // has a row's D elements, the others take the next parts.
 template <typename T, int D>
-__global__ void __launch_bounds__(256) join_kernel(Attend a, int chunk_rows, int parts) {
+__global__ void __launch_bounds__(256) join_kernel(Attend a, int chunk_rows) {
   constexpr int kLanes = D / 4, kAtOnce = 256 / kLanes;      // 16, 24, 32 or 64 threads a part
   __shared__ int64_t ends[SPQR_MAX_REQUESTS];
   __shared__ int64_t wave_sums[4];
   __shared__ float so[kAtOnce][D], sm[kAtOnce], sl[kAtOnce];
   const int tid = threadIdx.x;
   const int64_t work = scan_requests(a, chunk_rows, ends, wave_sums);
-  const int64_t part = part_size(work, parts);
+  const int64_t part = part_size(a, work);
   for (int64_t cut = blockIdx.x + 1; cut * part < work; cut += gridDim.x) {
     const int64_t x = cut * part;
     const int r = find_request(ends, a.requests, x);
     const Request rq = request_of(a, r, chunk_rows);
     const int64_t first = r == 0 ? 0 : ends[r - 1];
-    const int64_t pair = (x - first) / rq.tiles, from = first + pair * rq.tiles, to = from + rq.tiles;
+    const int pair = which_pair(x - first, rq.tiles);
+    const int64_t from = first + (int64_t)pair * rq.tiles, to = from + rq.tiles;
     if (x == from || x - part > from) continue;                // divides nothing; not the first cut
-    const int h = (int)(pair / rq.chunks), chunk = (int)(pair - (int64_t)h * rq.chunks);
+    const int h = pair / rq.chunks, chunk = pair - h * rq.chunks;
     const int row0 = chunk * chunk_rows, live_rows = min(rq.rows * a.group - row0, chunk_rows);
-    const int64_t w0 = cut - 1, count = (to - 1) / part - w0 + 1;
+    const int64_t w0 = cut - 1, count = parts_to(to - 1, part) - w0;
     const int mine = tid / kLanes, d = (tid - mine * kLanes) * 4;
     for (int row = blockIdx.y; row < live_rows; row += gridDim.y) {
       float best = -INFINITY, all = 0.f;
@@ -495,7 +553,7 @@ __global__ void __launch_bounds__(256) join_kernel(Attend a, int chunk_rows, int
           y1 = fmaf(c, so[i][2 * tid + 1], y1);
         }
         const float c = l == 0.f ? 0.f : 1.f / l;
-        const int full = row0 + row, tok = full / a.group;
+        const int full = row0 + row, tok = token_of(a, full);
         T* out = static_cast<T*>(a.out) + (int64_t)(rq.first_row + tok) * a.out_stride + (h * a.group + full - tok * a.group) * D + 2 * tid;
         *reinterpret_cast<uint32_t*>(out) = l == 0.f ? 0 : pack<T>(y0 * c, y1 * c);
       }
@@ -513,7 +571,7 @@ hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st) {
   else return hipErrorInvalidValue;
   const hipError_t e = hipGetLastError();
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((join_kernel<T, D>), dim3(p.join_x, p.join_y), block, 0, st, a, p.rows, p.workgroups);
+  hipLaunchKernelGGL((join_kernel<T, D>), dim3(p.join_x, p.join_y), block, 0, st, a, p.rows);
   return hipGetLastError();
 }
 

@@ -69,6 +69,9 @@ extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const vo
   a.requests = s->requests; a.tokens = s->tokens; a.kv_heads = s->kv_heads; a.group = s->heads / s->kv_heads;
   a.log_page = __builtin_ctz(s->page); a.pages = s->pages; a.max_pages = s->max_pages; a.words = s->mask_words;
   a.scale2 = s->scale * 1.4426950408889634f;
+  a.inv_group = 1.0f / (float)a.group;
+  a.workgroups = p.workgroups;
+  a.inv_workgroups = 1.0 / p.workgroups;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const hipError_t e = s->dtype == SPQR_F16 ? launch<_Float16>(s->head_dim, a, p, st) : launch<__bf16>(s->head_dim, a, p, st);
   return e == hipSuccess ? SPQR_OK : SPQR_ERR_HIP;

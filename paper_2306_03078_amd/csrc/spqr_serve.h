@@ -26,7 +26,7 @@ inline int check_cache(const spqr_step_t* s) {
   if (rc) return rc;
   if (s->dtype != SPQR_F16 && s->dtype != SPQR_BF16) return SPQR_ERR_DTYPE;
   if (s->head_dim != 64 && s->head_dim != 96 && s->head_dim != 128 && s->head_dim != 256) return SPQR_ERR_PARAM;
-  if (s->kv_heads < 1 || s->heads < 1 || s->heads > 65535 || s->heads % s->kv_heads != 0 || s->layers < 1) return SPQR_ERR_SHAPE;
+  if (s->kv_heads < 1 || s->heads < 1 || s->heads > 1024 || s->heads % s->kv_heads != 0 || s->layers < 1) return SPQR_ERR_SHAPE;
   if (!s->k || !s->v) return SPQR_ERR_NULL;
   if (!aligned(s->k, 16) || !aligned(s->v, 16)) return SPQR_ERR_ALIGN;
   return SPQR_OK;
