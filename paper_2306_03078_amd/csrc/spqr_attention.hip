@@ -18,12 +18,13 @@ static AttendPlan plan_attend(const spqr_step_t* s) {
   const int most = s->head_dim == 256 ? 32 : 64;
   p.rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
   p.workgroups = p.rows == 64 ? 256 : 512;
-  p.join_x = p.workgroups - 1;
-  p.join_y = (int)min(rows, (int64_t)4);
+  p.join_y = (int)((min(rows, (int64_t)p.rows) + 3) / 4);
   return p;
 }
 
-static int64_t workspace_bytes(const AttendPlan& p, int D) { return 2ll * p.workgroups * p.rows * (D + 2) * 4; }
+static int64_t workspace_bytes(const AttendPlan& p, int D) {
+  return (int64_t)p.workgroups * sizeof(Join) + 2ll * p.workgroups * p.rows * (D + 2) * 4;
+}
 
 template <typename T>
 static hipError_t launch(int D, const Attend& a, const AttendPlan& p, hipStream_t st) {
@@ -64,7 +65,8 @@ extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const vo
   a.k = static_cast<const char*>(s->k) + layer * layer_bytes;
   a.v = static_cast<const char*>(s->v) + layer * layer_bytes;
   a.cached = s->cached; a.table = s->table; a.q_start = s->q_start; a.mask = s->mask;
-  a.part_o = static_cast<float*>(s->workspace);
+  a.joins = static_cast<Join*>(s->workspace);
+  a.part_o = reinterpret_cast<float*>(a.joins + p.workgroups);
   a.part_ml = a.part_o + 2ll * p.workgroups * p.rows * s->head_dim;
   a.requests = s->requests; a.tokens = s->tokens; a.kv_heads = s->kv_heads; a.group = s->heads / s->kv_heads;
   a.log_page = __builtin_ctz(s->page); a.pages = s->pages; a.max_pages = s->max_pages; a.words = s->mask_words;
