@@ -25,7 +25,7 @@
 
 namespace spqr_srv {
 
-struct Join {                    // what a workgroup's cut leaves for join_kernel; parts = 0: nothing
+struct Join {                    // what the cut behind a workgroup divides; parts = 0: nothing
   int parts, slot, first_row, row0, live_rows, h, unused[2];
 };
 
@@ -38,19 +38,21 @@ struct Attend {
   Join* joins;                   // [workgroups]
   float *part_o, *part_ml;       // [2 * workgroups][rows of a chunk][D], [...][2]: reference, sum
   int requests, tokens, group, kv_heads, log_page, pages, max_pages, words;
-  float scale2;                  // scale * log2(e)
+  float scale2;                  // |scale| * log2(e)
+  uint32_t turn;                 // 0x80008000 where scale < 0: queries change their signs
   float inv_group;
   int workgroups;
+  int chunk_rows, start;         // of a chunk; places of the line in front of its tiles
   double inv_workgroups;
 };
 
 struct AttendPlan {              // of a launch; host
-  int rows;                      // of a chunk: 16 * MT
   int workgroups;
-  int join_y;                    // workgroups of join_kernel a cut, four rows each at a time
+  bool by_chunk;                 // join_kernel: workgroups for chunks, not for cuts
+  int join_x, join_y;
 };
 
-// D = 64, 96, 128, 256; T = _Float16, __bf16.  rows: 16, 32 or 64 (D = 256: 32 at most).
+// D = 64, 96, 128, 256; T = _Float16, __bf16.  a.chunk_rows: 16, 32, 48 or 64 (D = 256: 32 at most).
 template <typename T, int D> hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st);
 
 constexpr int kTile = 32;        // keys
@@ -112,15 +114,11 @@ __device__ __forceinline__ Request request_of(const Attend& a, int r) {
 }
 
 __device__ __forceinline__ int tiles_of(const Request& x) { return (x.keys + kTile - 1) / kTile; }
-template <int MT>
-__device__ __forceinline__ int chunks_of(const Attend& a, const Request& x) { return (x.rows * a.group + 16 * MT - 1) / (16 * MT); }
+__device__ __forceinline__ int chunks_of(const Attend& a, const Request& x) { return (x.rows * a.group + a.chunk_rows - 1) / a.chunk_rows; }
 
-// What a (key head, chunk) costs beside its tiles, in tiles: its start and end were measured to take as long.
-template <int MT> constexpr int kStart = MT == 1 ? 4 : MT == 2 ? 8 : 16;
-
-// The requests, and inclusive prefix sums of their parts of the line, in LDS; returns the line's length.  All 256 threads;
-// ends with a barrier.
-template <int MT>
+// The requests, and inclusive prefix sums of their parts of the line, in LDS; returns the line's length.  A (key head, chunk) has
+// a place for each of its tiles, and a.start in front of them for what it costs beside them.  All 256
+// threads; ends with a barrier.
 __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Request* requests, int64_t* wave_sums) {
   const int tid = threadIdx.x, lane = tid & 63, each = (a.requests + 255) / 256;
   int64_t sum = 0;
@@ -130,7 +128,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Requ
     if (r >= a.requests) break;
     const Request x = request_of(a, r);
     requests[r] = x;
-    ends[r] = sum += x.rows == 0 ? 0 : (int64_t)(tiles_of(x) + kStart<MT>) * chunks_of<MT>(a, x) * a.kv_heads;
+    ends[r] = sum += x.rows == 0 ? 0 : (int64_t)(tiles_of(x) + a.start) * chunks_of(a, x) * a.kv_heads;
   }
   int64_t upto = sum;
   for (int d = 1; d < 64; d <<= 1) {
@@ -140,6 +138,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Requ
   if (lane == 63) wave_sums[tid >> 6] = upto;
   __syncthreads();
   int64_t before = upto - sum, all = 0;
+#pragma unroll
   for (int w = 0; w < 4; ++w) {
     if (w < tid >> 6) before += wave_sums[w];
     all += wave_sums[w];
@@ -202,20 +201,29 @@ struct Segment {
   int64_t line;                              // place of its first tile
 };
 
+// max(a, b, c) as the instruction has it.  (fmaxf makes each operand pass through an instruction of its own first, lest it be a
+// signalling NaN; a NaN score makes its row NaN through its sum.)
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  float r;
+  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+  return r;
+}
+
 template <typename T, int D, int MT>
 __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   constexpr int DC = D / 32;                 // 32-element pieces of a key
   constexpr int E = D / 16, EW = E / 2;      // elements and dwords of a value that a lane loads
   constexpr int kRows = 16 * MT;
+  constexpr int kParts = 4 / MT;             // wavefronts that share 16 rows' results at the end
   extern __shared__ __align__(16) Request requests[];        // [requests], then the ends of their parts of the line
   __shared__ int64_t wave_sums[4];
-  __shared__ float so[4][MT][E][4 / MT][64][MT];
+  __shared__ float so[4][MT][E][kParts][64][4 / kParts];
   __shared__ float sm[4][kRows], sl[4][kRows];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), x16 = lane & 15, g = lane >> 4;
   int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
   if (tid == 0) a.joins[blockIdx.x].parts = 0;
-  const int64_t line = lay_line<MT>(a, line_ends, requests, wave_sums);
+  const int64_t line = lay_line(a, line_ends, requests, wave_sums);
   const int64_t part = part_size(a, line);
   const int64_t begin = blockIdx.x * part, end = min(line, begin + part);
   if (begin >= end) return;
@@ -231,10 +239,10 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       x.rq = {uniform(packed.x), uniform(packed.y), uniform(packed.z), uniform(packed.w)};
       x.r = r;
       x.tiles = tiles_of(x.rq);
-      const int chunks = chunks_of<MT>(a, x.rq), cost = x.tiles + kStart<MT>;
+      const int chunks = chunks_of(a, x.rq), cost = x.tiles + a.start;
       const int64_t first = r == 0 ? 0 : uniform(line_ends[r - 1]);
       const int pair = which_pair(at - first, cost);
-      x.line = first + (int64_t)pair * cost + kStart<MT>;
+      x.line = first + (int64_t)pair * cost + a.start;
       x.h = pair / chunks;
       x.row0 = (pair - x.h * chunks) * kRows;
       x.live_rows = min(x.rq.rows * a.group - x.row0, kRows);
@@ -253,8 +261,11 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   // results meet in later.
   constexpr bool kShared = MT > 1;
   u32x4(*shared_q)[DC][64] = reinterpret_cast<u32x4(*)[DC][64]>(&so[0][0][0][0][0][0]);
-  u32x4 q[kShared ? 1 : MT][DC], kf[2][DC];
-  uint32_t vf[8][EW];
+  u32x4 q[kShared ? 1 : MT][DC];
+  // A wavefront that is alone on its SIMD has the keys and values of its next two tiles on their way, else of one.
+  constexpr int kAhead = MT > 1 && MT * D <= 384 ? 2 : 1;
+  u32x4 kf[kAhead][2][DC];
+  uint32_t vf[kAhead][8][EW];
   int token[MT], id0 = 0, id1 = 0;
   const uint32_t k_lane = x16 * D + 8 * g, v_lane = 4 * g * D + E * x16;
   const T *kh, *vh;
@@ -263,27 +274,27 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     i0 = table[min((t * kTile) >> a.log_page, a.max_pages - 1)];
     i1 = table[min((t * kTile + 16) >> a.log_page, a.max_pages - 1)];
   };
-  auto load_keys = [&](int t, int i0, int i1, uint32_t from) {
+  auto load_keys = [&](int b, int t, int i0, int i1, uint32_t from) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const T* base = kh + half_offset(u ? i1 : i0, t * kTile + 16 * u);
 #pragma unroll
-      for (int c = 0; c < DC; ++c) kf[u][c] = *reinterpret_cast<const u32x4*>(base + (from + 32 * c));
+      for (int c = 0; c < DC; ++c) kf[b][u][c] = *reinterpret_cast<const u32x4*>(base + (from + 32 * c));
     }
   };
-  auto load_values = [&](int t, int i0, int i1, uint32_t from) {
+  auto load_values = [&](int b, int t, int i0, int i1, uint32_t from) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const T* base = vh + half_offset(u ? i1 : i0, t * kTile + 16 * u);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        __builtin_memcpy(vf[4 * u + i], __builtin_assume_aligned(base + (from + i * D), E % 8 == 0 ? 16 : E % 4 == 0 ? 8 : 4), 4 * EW);
+        __builtin_memcpy(vf[b][4 * u + i], __builtin_assume_aligned(base + (from + i * D), E % 8 == 0 ? 16 : E % 4 == 0 ? 8 : 4), 4 * EW);
     }
   };
   auto load_tile = [&](int t) {
     page_ids(t, id0, id1);
-    load_keys(t, id0, id1, k_lane);
-    load_values(t, id0, id1, v_lane);
+    load_keys(0, t, id0, id1, k_lane);
+    load_values(0, t, id0, id1, v_lane);
   };
   // a segment's queries and this wavefront's first tile; a row is (token, query head of the group)
   auto open = [&](const Segment& x) {
@@ -295,7 +306,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       const int row = x.row0 + min(16 * m + x16, x.live_rows - 1), tok = token_of(a, row);
       const T* from = static_cast<const T*>(a.q) + (int64_t)(x.rq.first_row + tok) * a.q_stride + (x.h * a.group + row - tok * a.group) * D + 8 * g;
       const u32x4 v = *reinterpret_cast<const u32x4*>(from + 32 * c);
-      return 16 * m + x16 < x.live_rows ? v : u32x4{0, 0, 0, 0};
+      return 16 * m + x16 < x.live_rows ? v ^ a.turn : u32x4{0, 0, 0, 0};
     };
 #pragma unroll
     for (int m = 0; m < MT; ++m) token[m] = 16 * m + x16 < x.live_rows ? token_of(a, x.row0 + 16 * m + x16) : -1;
@@ -329,13 +340,19 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       for (int n = 0; n < E; ++n) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
     }
 
-    // the steps of a tile
+    // The steps of a tile.  All 16 * MT rows are computed, also those that are none: straight code, in which the matrix cores'
+    // work and the rest alternate as written (a wavefront issues in order, and on chunks of 64 rows it is alone on its
+    // SIMD: what is not between two products waits for them).
     f32x4 s[MT][2];
+    u32x4 vt[E];
     uint32_t p[MT][4], seen[MT];
-    auto scores = [&] {
+    auto transpose = [&](int b, int k) {       // the k-th of 4 E exchanges
+      const int n = k / 4, j = k % 4;
+      vt[n][j] = __builtin_amdgcn_perm(vf[b][2 * j + 1][n / 2], vf[b][2 * j][n / 2], n & 1 ? 0x07060302 : 0x05040100);
+    };
+    auto scores = [&](int b) {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        if (m > 0 && 16 * m >= live_rows) continue;
         u32x4 query[DC];
 #pragma unroll
         for (int c = 0; c < DC; ++c) query[c] = kShared ? shared_q[m][c][lane] : q[kShared ? 0 : m][c];
@@ -343,57 +360,65 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         for (int u = 0; u < 2; ++u) {
           s[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < DC; ++c) s[m][u] = Matrix<T>::product(kf[u][c], query[c], s[m][u]);
+          for (int c = 0; c < DC; ++c) s[m][u] = Matrix<T>::product(kf[b][u][c], query[c], s[m][u]);
         }
       }
     };
-    auto probabilities = [&](auto masked_tile) {
+    auto references = [&](auto masked_tile) {  // where scores are too large for a row's reference, a new one
       constexpr bool masked = decltype(masked_tile)::value;
+      float most[MT];
+      bool moves = false;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        if (m > 0 && 16 * m >= live_rows) continue;
-        float z[8];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = s[m][j >> 2][j & 3] * a.scale2;
         if constexpr (masked) {
 #pragma unroll
-          for (int j = 0; j < 8; ++j) z[j] = seen[m] >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1 ? z[j] : -INFINITY;
+          for (int j = 0; j < 8; ++j)
+            if (!(seen[m] >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1)) s[m][j >> 2][j & 3] = -INFINITY;
         }
-        float most = fmaxf(fmaxf(fmaxf(z[0], z[1]), fmaxf(z[2], z[3])), fmaxf(fmaxf(z[4], z[5]), fmaxf(z[6], z[7])));
-        if (__any(most > top[m] + 8.f)) {
-          most = fmaxf(most, __shfl_xor(most, 16));
-          most = fmaxf(most, __shfl_xor(most, 32));
-          const float now = most > top[m] + 8.f ? most : top[m];
+        const f32x4 x = s[m][0], y = s[m][1];
+        most[m] = max3(max3(x[0], x[1], x[2]), max3(x[3], y[0], y[1]), max3(y[2], y[3], y[3])) * a.scale2;
+        moves |= most[m] > top[m] + 8.f;
+      }
+      if (__any(moves)) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) {
+          most[m] = fmaxf(most[m], __shfl_xor(most[m], 16));
+          most[m] = fmaxf(most[m], __shfl_xor(most[m], 32));
+          const float now = most[m] > top[m] + 8.f ? most[m] : top[m];
           const float back = now == top[m] ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
           top[m] = now;
           sum[m] *= back;
 #pragma unroll
-          for (int n = 0; n < E; ++n) o[m][n] *= back;
+          for (int n = 0; n < E; ++n) {
+            o[m][n] *= back;
+            if (MT > 1 && n % 2) __builtin_amdgcn_sched_barrier(0);    // few of them out of the accumulation registers at a time
+          }
         }
-        const float ref = top[m] == -INFINITY ? 0.f : top[m];
-#pragma unroll
-        for (int j = 0; j < 8; ++j) z[j] = __builtin_amdgcn_exp2f(z[j] - ref);
-        sum[m] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
-#pragma unroll
-        for (int j = 0; j < 4; ++j) p[m][j] = pack<T>(z[2 * j], z[2 * j + 1]);
       }
-
     };
-    u32x4 vt[E];
-    auto transpose = [&] {
-#pragma unroll
-      for (int n = 0; n < E; ++n)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) vt[n][j] = __builtin_amdgcn_perm(vf[2 * j + 1][n / 2], vf[2 * j][n / 2], n & 1 ? 0x07060302 : 0x05040100);
+    auto exponentials = [&](int m, int k) {    // the k-th pair of keys of rows m
+      const float ref = top[m] == -INFINITY ? 0.f : top[m];
+      const float one = __builtin_amdgcn_exp2f(fmaf(s[m][k >> 1][2 * (k & 1)], a.scale2, -ref));
+      const float two = __builtin_amdgcn_exp2f(fmaf(s[m][k >> 1][2 * (k & 1) + 1], a.scale2, -ref));
+      sum[m] += one + two;
+      p[m][k] = pack<T>(one, two);
     };
-    auto outputs = [&] {
+    auto output = [&](int m, int n) {
+      const u32x4 b = {p[m][0], p[m][1], p[m][2], p[m][3]};
+      o[m][n] = Matrix<T>::product(vt[n], b, o[m][n]);
+    };
+    auto outputs = [&] {                       // O^T of one row tile beside the probabilities of the next
 #pragma unroll
-      for (int m = 0; m < MT; ++m) {
-        if (m > 0 && 16 * m >= live_rows) continue;
-        const u32x4 b = {p[m][0], p[m][1], p[m][2], p[m][3]};
+      for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int n = 0; n < E; ++n) o[m][n] = Matrix<T>::product(vt[n], b, o[m][n]);
-      }
+        for (int n = 0; n < E; ++n) {
+          if (MT > 1) __builtin_amdgcn_sched_barrier(0);
+          output(m, n);
+          if (m + 1 < MT) {
+#pragma unroll
+            for (int k = n * 4 / E; k < (n + 1) * 4 / E; ++k) exponentials(m + 1, k);
+          }
+        }
     };
 
     // Tiles of cached keys that are all there.  The next tile's loads go into the registers that this one's products have read;
@@ -403,32 +428,64 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     int t = now.t0 + wave;
     if (t < plain_end) {
       const int last = t1 - 1;
-      int next0, next1, later0, later1;      // page ids are on their way for two tiles
-      page_ids(min(t + 4, last), next0, next1);
-      page_ids(min(t + 8, last), later0, later1);
-      while (t < plain_end && there(id0) && there(id1)) {
-        const bool more = t + 4 < t1;
-        const int following = min(t + 4, last);
-        scores();
+      int ids[kAhead + 2][2];                // page ids are on their way for a tile more; [0]: this tile's
+      ids[0][0] = id0;
+      ids[0][1] = id1;
+#pragma unroll
+      for (int i = 1; i < kAhead + 2; ++i) page_ids(min(t + 4 * i, last), ids[i][0], ids[i][1]);
+      if constexpr (kAhead == 2) {
+        load_keys(1, min(t + 4, last), ids[1][0], ids[1][1], t + 4 < t1 ? k_lane : 0);
+        load_values(1, min(t + 4, last), ids[1][0], ids[1][1], t + 4 < t1 ? v_lane : 0);
+      }
+      auto step = [&](int b) {               // false: the tile is for the other loop
+        if (!(t < plain_end && there(ids[0][0]) && there(ids[0][1]))) return false;
+        const bool more = t + 4 * kAhead < t1;
+        const int following = min(t + 4 * kAhead, last);
+        scores(b);
         __builtin_amdgcn_sched_barrier(0);
-        load_keys(following, next0, next1, more ? k_lane : 0);
-        probabilities(std::false_type());
-        transpose();
+        load_keys(b, following, ids[kAhead][0], ids[kAhead][1], more ? k_lane : 0);
+        references(std::false_type());
+#pragma unroll
+        for (int k = 0; k < 4; ++k) exponentials(0, k);
+#pragma unroll
+        for (int k = 0; k < 4 * E; ++k) transpose(b, k);
         __builtin_amdgcn_sched_barrier(0);
-        load_values(following, next0, next1, more ? v_lane : 0);
+        load_values(b, following, ids[kAhead][0], ids[kAhead][1], more ? v_lane : 0);
         outputs();
         t += 4;
-        id0 = next0;
-        id1 = next1;
-        next0 = later0;
-        next1 = later1;
-        page_ids(min(t + 8, last), later0, later1);
+#pragma unroll
+        for (int i = 0; i <= kAhead; ++i) {
+          ids[i][0] = ids[i + 1][0];
+          ids[i][1] = ids[i + 1][1];
+        }
+        page_ids(min(t + 4 * (kAhead + 1), last), ids[kAhead + 1][0], ids[kAhead + 1][1]);
+        return true;
+      };
+      bool odd = false;
+      while (step(0)) {
+        if constexpr (kAhead == 2) {
+          odd = true;
+          if (!step(1)) break;
+          odd = false;
+        }
       }
+      if (kAhead == 2 && odd && t < t1) {
+#pragma unroll
+        for (int u = 0; u < 2; ++u)
+#pragma unroll
+          for (int c = 0; c < DC; ++c) kf[0][u][c] = kf[kAhead - 1][u][c];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+#pragma unroll
+          for (int e = 0; e < EW; ++e) vf[0][j][e] = vf[kAhead - 1][j][e];
+      }
+      id0 = ids[0][0];
+      id1 = ids[0][1];
     }
     // the last cached keys, the new ones, and what lies on and behind pages that are not there
     while (t < t1) {
       const int key0 = t * kTile;
-      scores();
+      scores(0);
       {
         const bool there0 = there(id0) && key0 >> a.log_page < a.max_pages, there1 = there(id1) && (key0 + 16) >> a.log_page < a.max_pages;
         const int left = rq.keys - key0;
@@ -461,10 +518,14 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         for (int j = 0; j < 8; ++j) {
           const bool on = exist >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1;
 #pragma unroll
-          for (int e = 0; e < EW; ++e) vf[j][e] = on ? vf[j][e] : 0;
+          for (int e = 0; e < EW; ++e) vf[0][j][e] = on ? vf[0][j][e] : 0;
         }
       }
-      probabilities(std::true_type());
+      references(std::true_type());
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int k = 0; k < 4; ++k) exponentials(m, k);
       {
         // Infinities and NaN among the values: 0 * inf would reach rows that do not see the key.  Such a key is taken out of
         // the matrix product and added by the rows that see it; the probabilities pass through this wavefront's part of `so`.
@@ -474,7 +535,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
           bool mine = false;
 #pragma unroll
           for (int e = 0; e < EW; ++e)
-            mine |= (vf[j][e] & Matrix<T>::kExponent) == Matrix<T>::kExponent || (vf[j][e] >> 16 & Matrix<T>::kExponent) == Matrix<T>::kExponent;
+            mine |= (vf[0][j][e] & Matrix<T>::kExponent) == Matrix<T>::kExponent || (vf[0][j][e] >> 16 & Matrix<T>::kExponent) == Matrix<T>::kExponent;
           const uint64_t votes = __ballot(mine);
 #pragma unroll
           for (int k = 0; k < 4; ++k) bad |= (votes >> (16 * k) & 0xFFFF) != 0 ? 1u << (16 * (j >> 2) + 4 * k + (j & 3)) : 0;
@@ -486,10 +547,10 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
             const T* v = vh + half_offset(key < 16 ? id0 : id1, key0 + (key & 16)) + (key & 15) * D + E * 4 * g;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
-              const uint32_t mine = j < 4 ? (j < 2 ? p[m][0] : p[m][1]) : (j < 6 ? p[m][2] : p[m][3]);
-              const uint32_t both = __shfl(mine, from);
+              const uint32_t b0 = __shfl(p[m][0], from), b1 = __shfl(p[m][1], from), b2 = __shfl(p[m][2], from), b3 = __shfl(p[m][3], from);
+              const uint32_t both = j < 4 ? (j < 2 ? b0 : b1) : (j < 6 ? b2 : b3);
               const float weight = (float)__builtin_bit_cast(T, (uint16_t)(j & 1 ? both >> 16 : both));
-              if (16 * m < live_rows && (seen[m] >> key & 1)) {
+              if (seen[m] >> key & 1) {
 #pragma unroll
                 for (int n = 0; n < E; ++n)
 #pragma unroll
@@ -501,12 +562,16 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
           for (int j = 0; j < 8; ++j) {
             const bool out = bad >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1;
 #pragma unroll
-            for (int e = 0; e < EW; ++e) vf[j][e] = out ? 0 : vf[j][e];
+            for (int e = 0; e < EW; ++e) vf[0][j][e] = out ? 0 : vf[0][j][e];
           }
         }
       }
-      transpose();
-      outputs();
+#pragma unroll
+      for (int k = 0; k < 4 * E; ++k) transpose(0, k);
+#pragma unroll
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int n = 0; n < E; ++n) output(m, n);
       t += 4;
       if (t < t1) load_tile(t);
     }
@@ -517,32 +582,34 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     work = next_segment(now);
     if (kEarly && work) open(now);
 
-    // The wavefronts add up in LDS: each takes 16 rows (MT = 4), or a half (2) or a quarter (1) of their elements: those that
-    // a lane holds in i = MT * (wave / MT) .. of a result, E neighbouring elements an i.
+    // The wavefronts add up in LDS: each takes a 16-row tile, or as many of its elements as kParts leave it: those that a lane
+    // holds in i = i0 .. of a result, E neighbouring elements an i.
+    constexpr int kI = 4 / kParts;
+    const int tile = wave % MT, i0 = wave / MT * kI;
     const bool whole = done.t0 == 0 && done.t1 == done.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (begin >= done.line ? 0 : 1);
     __syncthreads();
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
-      if (m > 0 && 16 * m >= live_rows) continue;
+      const int row = 16 * m + x16;
       float l = sum[m];
       l += __shfl_xor(l, 16);
       l += __shfl_xor(l, 32);
-      if (g == 0) { sm[wave][16 * m + x16] = top[m]; sl[wave][16 * m + x16] = l; }
-      if (16 * m + x16 < live_rows) {
+      if (g == 0) { sm[wave][row] = top[m]; sl[wave][row] = l; }
+      if (row < live_rows) {
 #pragma unroll
         for (int n = 0; n < E; ++n)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) so[wave][m][n][i / MT][lane][i % MT] = o[m][n][i];
+          for (int i = 0; i < 4; ++i) so[wave][m][n][i / kI][lane][i % kI] = o[m][n][i];
       }
     }
     __syncthreads();
-    const int in_chunk = 16 * (wave % MT) + x16;
-    if (in_chunk < live_rows) {
+    const int in_chunk = 16 * tile + x16;
+    if (wave / MT < kParts && in_chunk < live_rows) {
       const float best = fmaxf(fmaxf(sm[0][in_chunk], sm[1][in_chunk]), fmaxf(sm[2][in_chunk], sm[3][in_chunk]));
-      float y[MT][E], all = 0.f;
+      float y[kI][E], all = 0.f;
 #pragma unroll
-      for (int k = 0; k < MT; ++k)
+      for (int k = 0; k < kI; ++k)
 #pragma unroll
         for (int n = 0; n < E; ++n) y[k][n] = 0.f;
 #pragma unroll
@@ -552,15 +619,15 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
 #pragma unroll
         for (int n = 0; n < E; ++n)
 #pragma unroll
-          for (int k = 0; k < MT; ++k) y[k][n] = fmaf(c, so[w][wave % MT][n][wave / MT][lane][k], y[k][n]);
+          for (int k = 0; k < kI; ++k) y[k][n] = fmaf(c, so[w][tile][n][wave / MT][lane][k], y[k][n]);
       }
-      const int d = E * (4 * g + MT * (wave / MT));
+      const int d = E * (4 * g + i0);
       if (whole) {
         const int row = done.row0 + in_chunk, tok = token_of(a, row);
         const float c = 1.f / all;
         T* to = static_cast<T*>(a.out) + (int64_t)(done.rq.first_row + tok) * a.out_stride + (done.h * a.group + row - tok * a.group) * D + d;
 #pragma unroll
-        for (int k = 0; k < MT; ++k) {
+        for (int k = 0; k < kI; ++k) {
 #pragma unroll
           for (int n = 0; n < E; ++n) y[k][n] = all == 0.f ? 0.f : y[k][n] * c;
           store_run<T, E>(to + E * k, y[k]);
@@ -568,10 +635,10 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       } else {
         float* to = a.part_o + (slot * kRows + in_chunk) * D + d;
 #pragma unroll
-        for (int k = 0; k < MT; ++k)
+        for (int k = 0; k < kI; ++k)
 #pragma unroll
           for (int n = 0; n < E; n += 2) *reinterpret_cast<float2*>(to + E * k + n) = make_float2(y[k][n], y[k][n + 1]);
-        if (wave / MT == 0 && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * (slot * kRows + in_chunk)) = make_float2(best, all);
+        if (i0 == 0 && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * (slot * kRows + in_chunk)) = make_float2(best, all);
       }
     }
     if (tid == 0 && done.t0 == 0 && !whole) {  // the first part of what the cut behind this workgroup divides
@@ -588,50 +655,95 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   }
 }
 
-// Adds the parts of what the cut behind workgroup x divided, in their order: a wavefront a row.
-template <typename T, int D>
-__global__ void __launch_bounds__(256) join_kernel(Attend a, int chunk_rows) {
+// Adds the parts of what the cuts divided, in their order, and writes the rows out.  Workgroup x takes the cut behind workgroup x of
+// the attention, a wavefront a row: most cuts divide something.  Where there are few chunks, each of them in many parts
+// (by_chunk), it takes the x-th chunk, and its wavefronts every fourth part of a row.
+template <typename T, int D, bool by_chunk>
+__global__ void __launch_bounds__(256) join_kernel(Attend a) {
   constexpr int PE = D >= 128 ? D / 64 : D == 96 ? 2 : 1;      // elements a lane
+  __shared__ float meet[4][D + 2];
+  __shared__ int64_t wave_sums[4];
+  extern __shared__ __align__(16) Request requests[];
   const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-  const Join j = a.joins[blockIdx.x];
-  if (j.parts == 0) return;
   const int d = min(lane * PE, D - PE);      // (D = 96: the last lanes repeat the last elements)
-  for (int row = 4 * blockIdx.y + wave; row < j.live_rows; row += 4 * gridDim.y) {
-    // the parts behind the first lie in the first slots of the next workgroups
-    auto place = [&](int i) { return (int64_t)(i == 0 ? j.slot : 2 * ((int)blockIdx.x + i)) * chunk_rows + row; };
-    float best = -INFINITY, all = 0.f, y[PE];
-#pragma unroll
-    for (int e = 0; e < PE; ++e) y[e] = 0.f;
-    for (int i0 = 0; i0 < j.parts; i0 += 64) {
-      const bool have = i0 + lane < j.parts;
-      const float2 ml = have ? *reinterpret_cast<const float2*>(a.part_ml + 2 * place(i0 + lane)) : make_float2(-INFINITY, 0.f);
-      float most = ml.x;
-      for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
-      const float top = fmaxf(best, most);
-      const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top), back = best == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(best - top);
-      float l = c * ml.y;
-      for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k);
-      all = all * back + l;
-      best = top;
-#pragma unroll
-      for (int e = 0; e < PE; ++e) y[e] *= back;
-      const int n = min(64, j.parts - i0);
-#pragma unroll 8
-      for (int i = 0; i < n; ++i) {
-        const float w = __shfl(c, i);
-        float v[PE];
-        __builtin_memcpy(v, __builtin_assume_aligned(a.part_o + place(i0 + i) * D + d, 4 * PE), 4 * PE);
-#pragma unroll
-        for (int e = 0; e < PE; ++e) y[e] = fmaf(w, v[e], y[e]);
-      }
+  int from = blockIdx.x;
+  int64_t part = 0, at = 0;
+  int r = 0;
+  int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
+  if constexpr (by_chunk) {
+    part = part_size(a, lay_line(a, line_ends, requests, wave_sums));
+    at = blockIdx.x;                         // of the chunks of request r and those behind it
+  }
+  for (;;) {
+    if constexpr (by_chunk) {
+      int64_t chunks;
+      while (r < a.requests && at >= (chunks = (int64_t)chunks_of(a, requests[r]) * a.kv_heads)) { at -= chunks; ++r; }
+      if (r >= a.requests) return;
+      const int tiles = tiles_of(requests[r]);
+      const int64_t first = (r == 0 ? 0 : line_ends[r - 1]) + at * (tiles + a.start) + a.start;
+      at += gridDim.x;
+      from = (int)part_of(uniform(first), part);
+      if (part_of(uniform(first + tiles - 1), part) == from) continue;     // whole
     }
-    const float c = 1.f / all;
-    const int full = j.row0 + row, tok = token_of(a, full);
-    T out[PE];
+    const Join j = a.joins[from];
+    if (j.parts == 0) return;
+    const int parts_step = by_chunk ? 4 : 1, part0 = by_chunk ? wave : 0;
+    for (int row = by_chunk ? (int)blockIdx.y : 4 * (int)blockIdx.y + wave; row < j.live_rows; row += by_chunk ? (int)gridDim.y : 4 * (int)gridDim.y) {
+      // the parts behind the first lie in the first slots of the next workgroups
+      auto place = [&](int i) { return (int64_t)(i == 0 ? j.slot : 2 * (from + i)) * a.chunk_rows + row; };
+      float best = -INFINITY, all = 0.f, y[PE];
 #pragma unroll
-    for (int e = 0; e < PE; ++e) out[e] = (T)(all == 0.f ? 0.f : y[e] * c);
-    T* to = static_cast<T*>(a.out) + (int64_t)(j.first_row + tok) * a.out_stride + (j.h * a.group + full - tok * a.group) * D + d;
-    __builtin_memcpy(__builtin_assume_aligned(to, 2 * PE), out, 2 * PE);
+      for (int e = 0; e < PE; ++e) y[e] = 0.f;
+      for (int i0 = part0; i0 < j.parts; i0 += 64 * parts_step) {
+        const int own = i0 + lane * parts_step;
+        const float2 ml = own < j.parts ? *reinterpret_cast<const float2*>(a.part_ml + 2 * place(own)) : make_float2(-INFINITY, 0.f);
+        float most = ml.x;
+        for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+        const float top = fmaxf(best, most);
+        const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top), back = best == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(best - top);
+        float l = c * ml.y;
+        for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k);
+        all = all * back + l;
+        best = top;
+#pragma unroll
+        for (int e = 0; e < PE; ++e) y[e] *= back;
+        const int n = min(64, (j.parts - i0 + parts_step - 1) / parts_step);
+#pragma unroll 16
+        for (int i = 0; i < n; ++i) {
+          const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), i));
+          float v[PE];
+          __builtin_memcpy(v, __builtin_assume_aligned(a.part_o + place(i0 + i * parts_step) * D + d, 4 * PE), 4 * PE);
+#pragma unroll
+          for (int e = 0; e < PE; ++e) y[e] = fmaf(w, v[e], y[e]);
+        }
+      }
+      if constexpr (by_chunk) {
+        __syncthreads();
+#pragma unroll
+        for (int e = 0; e < PE; ++e) meet[wave][d + e] = y[e];
+        if (lane == 0) { meet[wave][D] = best; meet[wave][D + 1] = all; }
+        __syncthreads();
+        if (wave != 0) continue;
+        best = fmaxf(fmaxf(meet[0][D], meet[1][D]), fmaxf(meet[2][D], meet[3][D]));
+        all = 0.f;
+#pragma unroll
+        for (int e = 0; e < PE; ++e) y[e] = 0.f;
+        for (int w = 0; w < 4; ++w) {
+          const float c = meet[w][D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(meet[w][D] - best);
+          all = fmaf(c, meet[w][D + 1], all);
+#pragma unroll
+          for (int e = 0; e < PE; ++e) y[e] = fmaf(c, meet[w][d + e], y[e]);
+        }
+      }
+      const float c = 1.f / all;
+      const int full = j.row0 + row, tok = token_of(a, full);
+      T out[PE];
+#pragma unroll
+      for (int e = 0; e < PE; ++e) out[e] = (T)(all == 0.f ? 0.f : y[e] * c);
+      T* to = static_cast<T*>(a.out) + (int64_t)(j.first_row + tok) * a.out_stride + (j.h * a.group + full - tok * a.group) * D + d;
+      __builtin_memcpy(__builtin_assume_aligned(to, 2 * PE), out, 2 * PE);
+    }
+    if constexpr (!by_chunk) return;
   }
 }
 
@@ -645,11 +757,13 @@ static hipError_t launch_chunks(const Attend& a, const AttendPlan& p, hipStream_
 template <typename T, int D>
 hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st) {
   hipError_t e = hipErrorInvalidValue;
-  if (p.rows == 16) e = launch_chunks<T, D, 1>(a, p, st);
-  else if (p.rows == 32) e = launch_chunks<T, D, 2>(a, p, st);
-  else if constexpr (D < 256) e = launch_chunks<T, D, 4>(a, p, st);
+  if (a.chunk_rows == 16) e = launch_chunks<T, D, 1>(a, p, st);
+  else if (a.chunk_rows == 32) e = launch_chunks<T, D, 2>(a, p, st);
+  else if constexpr (D < 256) e = a.chunk_rows == 48 ? launch_chunks<T, D, 3>(a, p, st) : launch_chunks<T, D, 4>(a, p, st);
   if (e != hipSuccess) return e;
-  hipLaunchKernelGGL((join_kernel<T, D>), dim3(p.workgroups, p.join_y), dim3(256), 0, st, a, p.rows);
+  const size_t lds = (size_t)a.requests * (sizeof(int64_t) + sizeof(Request));
+  if (p.by_chunk) hipLaunchKernelGGL((join_kernel<T, D, true>), dim3(p.join_x, p.join_y), dim3(256), lds, st, a);
+  else hipLaunchKernelGGL((join_kernel<T, D, false>), dim3(p.join_x, p.join_y), dim3(256), 0, st, a);
   return hipGetLastError();
 }
 

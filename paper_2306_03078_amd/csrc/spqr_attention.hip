@@ -11,19 +11,26 @@ SPQR_ATTEND_EXTERN(96)
 SPQR_ATTEND_EXTERN(128)
 SPQR_ATTEND_EXTERN(256)
 
-// Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them.
-static AttendPlan plan_attend(const spqr_step_t* s) {
+// Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them.  The hint
+// only chooses; any rows are right with any chunks.
+static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   AttendPlan p;
   const int64_t rows = (int64_t)(s->max_fresh > 0 ? s->max_fresh : SPQR_MAX_FRESH) * (s->heads / s->kv_heads);
   const int most = s->head_dim == 256 ? 32 : 64;
-  p.rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : 64;
-  p.workgroups = p.rows == 64 ? 256 : 512;
-  p.join_y = (int)((min(rows, (int64_t)p.rows) + 3) / 4);
+  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : rows <= 64 ? 64 : 48;
+  a->start = a->chunk_rows == 16 ? 4 : a->chunk_rows == 32 ? 8 : 16;
+  // as many as run at once: two of four wavefronts a CU with 16 rows (one with D = 256), else one
+  p.workgroups = a->chunk_rows == 16 && s->head_dim < 256 ? 512 : 256;
+  const int64_t live = min(rows, (int64_t)a->chunk_rows);
+  const int64_t chunks = (int64_t)s->requests * s->kv_heads * ((rows + a->chunk_rows - 1) / a->chunk_rows);
+  p.by_chunk = chunks * 16 < p.workgroups;
+  p.join_x = p.by_chunk ? (int)chunks : p.workgroups;
+  p.join_y = (int)(p.by_chunk ? live : (live + 3) / 4);
   return p;
 }
 
-static int64_t workspace_bytes(const AttendPlan& p, int D) {
-  return (int64_t)p.workgroups * sizeof(Join) + 2ll * p.workgroups * p.rows * (D + 2) * 4;
+static int64_t workspace_bytes(const AttendPlan& p, int chunk_rows, int D) {
+  return (int64_t)p.workgroups * sizeof(Join) + 2ll * p.workgroups * chunk_rows * (D + 2) * 4;
 }
 
 template <typename T>
@@ -42,7 +49,10 @@ using namespace spqr_srv;
 
 extern "C" int64_t spqr_tree_attention_workspace_bytes(const spqr_step_t* s) {
   const int rc = check_cache(s);
-  return rc ? rc : workspace_bytes(plan_attend(s), s->head_dim);
+  if (rc) return rc;
+  Attend a;
+  const AttendPlan p = plan_attend(s, &a);
+  return workspace_bytes(p, a.chunk_rows, s->head_dim);
 }
 
 extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const void* q, int64_t q_stride, void* out, int64_t out_stride,
@@ -57,20 +67,21 @@ extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const vo
   if (!aligned(q, 16) || !aligned(out, 16) || q_stride % 8 != 0 || out_stride % 8 != 0 || !aligned(s->cached, 4) || !aligned(s->table, 4) ||
       !aligned(s->q_start, 4) || !aligned(s->mask, 8) || !aligned(s->workspace, 256))
     return SPQR_ERR_ALIGN;
-  const AttendPlan p = plan_attend(s);
-  if (s->workspace_bytes < workspace_bytes(p, s->head_dim)) return SPQR_ERR_WORKSPACE;
-  const int64_t layer_bytes = (int64_t)s->pages * s->kv_heads * s->page * s->head_dim * 2;
   Attend a;
+  const AttendPlan p = plan_attend(s, &a);
+  if (s->workspace_bytes < workspace_bytes(p, a.chunk_rows, s->head_dim)) return SPQR_ERR_WORKSPACE;
+  const int64_t layer_bytes = (int64_t)s->pages * s->kv_heads * s->page * s->head_dim * 2;
   a.q = q; a.out = out; a.q_stride = q_stride; a.out_stride = out_stride;
   a.k = static_cast<const char*>(s->k) + layer * layer_bytes;
   a.v = static_cast<const char*>(s->v) + layer * layer_bytes;
   a.cached = s->cached; a.table = s->table; a.q_start = s->q_start; a.mask = s->mask;
   a.joins = static_cast<Join*>(s->workspace);
   a.part_o = reinterpret_cast<float*>(a.joins + p.workgroups);
-  a.part_ml = a.part_o + 2ll * p.workgroups * p.rows * s->head_dim;
+  a.part_ml = a.part_o + 2ll * p.workgroups * a.chunk_rows * s->head_dim;
   a.requests = s->requests; a.tokens = s->tokens; a.kv_heads = s->kv_heads; a.group = s->heads / s->kv_heads;
   a.log_page = __builtin_ctz(s->page); a.pages = s->pages; a.max_pages = s->max_pages; a.words = s->mask_words;
-  a.scale2 = s->scale * 1.4426950408889634f;
+  a.scale2 = std::fabs(s->scale) * 1.4426950408889634f;
+  a.turn = s->scale < 0.f ? 0x80008000u : 0u;
   a.inv_group = 1.0f / (float)a.group;
   a.workgroups = p.workgroups;
   a.inv_workgroups = 1.0 / p.workgroups;

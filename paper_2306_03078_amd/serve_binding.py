@@ -70,8 +70,8 @@ class SpQRStep:
 
     k_cache, v_cache: [layers, pages, kv_heads, page, head_dim] float16 or bfloat16 device tensors (None for a step that
     is only planned: give page and pages).  heads: query heads.  requests, tokens, max_pages: sizes, where no array given says
-    them.  Any array of include/spqr_serve.h can be given by its name; the others are made here: empty requests, an
-    empty table, a ring with all pages free.  parent (int32 [tokens]) is None unless given, mask exists where mask_words > 0
+    them.  Any array of include/spqr_serve.h can be given by its name; the others are made here: empty requests, and an
+    empty table with a ring that has all pages (pool and ends are only made with a table).  parent (int32 [tokens]) is None unless given, mask exists where mask_words > 0
     or it is given.  rotary: float32 [positions, rotary_dim], cosines, then sines, or None.  scale: head_dim ** -0.5 if None.
     The step keeps the tensors alive and owns the attention's scratch: use it on one stream at a time."""
 
@@ -126,23 +126,30 @@ class SpQRStep:
         def on_device(a):
             return a.device == self.device
 
+        # the arrays that are not given, in one buffer
+        missing = [n for n in _ARRAYS if n not in given and n != "parent" and (n != "mask" or self.mask_words)
+                   and (n not in ("pool", "ends") or "table" not in given)]
+        sizes = [math.prod(_ARRAYS[n][1](self)) * (2 if _ARRAYS[n][0] == "int64" else 1) for n in missing]
+        places = [0]
+        for k in sizes:
+            places.append(places[-1] + -(-k // 64) * 64)
+        buffer = torch.zeros(places[-1], dtype=torch.int32, device=self.device)
+        for n, k, at in zip(missing, sizes, places):
+            dtype, shape = _ARRAYS[n]
+            given[n] = buffer[at:at + k].view(getattr(torch, dtype)).view(shape(self))
+        if "table" in missing:
+            given["table"].fill_(-1)
+        if "pool" in missing:
+            torch.arange(self.pages, dtype=torch.int32, device=self.device, out=given["pool"])
+        if "ends" in missing:
+            given["ends"][1] = self.pages
         for n, (dtype, shape) in _ARRAYS.items():
             a = given.get(n)
-            if a is None:
-                if n == "parent" or (n == "mask" and not self.mask_words):
-                    setattr(self, n, None)
-                    continue
-                a = torch.zeros(shape(self), dtype=getattr(torch, dtype), device=self.device)
-                if n == "table":
-                    a.fill_(-1)
-                elif n == "pool":
-                    torch.arange(self.pages, dtype=torch.int32, device=self.device, out=a)
-                elif n == "ends":
-                    a[1] = self.pages
-            if a.dtype != getattr(torch, dtype) or not a.is_contiguous() or tuple(a.shape) != shape(self) or not on_device(a):
-                raise ValueError(f"{n}: a contiguous {dtype} tensor {list(shape(self))} on {self.device}, not {a.dtype} {list(a.shape)} on {a.device}")
+            if a is not None:
+                if a.dtype != getattr(torch, dtype) or not a.is_contiguous() or tuple(a.shape) != shape(self) or not on_device(a):
+                    raise ValueError(f"{n}: a contiguous {dtype} tensor {list(shape(self))} on {self.device}, not {a.dtype} {list(a.shape)} on {a.device}")
+                setattr(d, n, a.data_ptr())
             setattr(self, n, a)
-            setattr(d, n, a.data_ptr())
         self.rotary = rotary
         if rotary is not None:
             if rotary.dtype != torch.float32 or rotary.dim() != 2 or not rotary.is_contiguous() or not on_device(rotary):
@@ -155,6 +162,9 @@ class SpQRStep:
                 raise SpQRError(need, "spqr_tree_attention_workspace_bytes")
             self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             d.workspace, d.workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
+        T, D = self.tokens, self.head_dim
+        self._q_like, self._kv_like = (((T, h, D), (h * D, D, 1)) for h in (self.heads, self.kv_heads))
+        self._q_of = torch.empty(1, dtype=self.dtype, device=self.device).expand(T, self.heads, D)
         self._rows = spqr_rows_t()
         self._rows_at = C.addressof(self._rows)
 
@@ -177,15 +187,20 @@ def spqr_cache_plan(step: SpQRStep, stream=None) -> SpQRStep:
     return step
 
 
-def _row_stride(x, tokens, heads, head_dim, name):
-    """Elements between the rows of [tokens, heads, head_dim] or [tokens, heads * head_dim], each of them contiguous."""
-    shape = x.shape
+def _row_stride(x, like, name):
+    """Elements between the rows of x: [tokens, heads, head_dim] or [tokens, heads * head_dim], each row contiguous.  like: the
+    shape and strides of the dense one."""
+    shape, strides = x.shape, x.stride()
+    if shape == like[0] and strides == like[1]:
+        return strides[0]
+    (tokens, heads, head_dim), row = like[0], like[1][0]
     if len(shape) == 3:
-        if shape[0] == tokens and shape[1] == heads and shape[2] == head_dim and x.stride(2) == 1 and (heads == 1 or x.stride(1) == head_dim):
-            return x.stride(0) if tokens > 1 else max(x.stride(0), heads * head_dim)
-    elif len(shape) == 2 and shape[0] == tokens and shape[1] == heads * head_dim and x.stride(1) == 1:
-        return x.stride(0) if tokens > 1 else max(x.stride(0), heads * head_dim)
-    raise ValueError(f"{name}: [{tokens}, {heads}, {head_dim}] with contiguous rows, not {list(shape)} with strides {list(x.stride())}")
+        fits = shape == like[0] and strides[2] == 1 and (heads == 1 or strides[1] == head_dim)
+    else:
+        fits = shape == (tokens, row) and strides[1] == 1
+    if not fits:
+        raise ValueError(f"{name}: [{tokens}, {heads}, {head_dim}] with contiguous rows, not {list(shape)} with strides {list(strides)}")
+    return strides[0] if tokens > 1 else max(strides[0], row)
 
 
 def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=None):
@@ -196,15 +211,14 @@ def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=N
     dtype = q.dtype
     if dtype not in _dtypes or k.dtype != dtype or v.dtype != dtype:
         raise ValueError(f"q, k, v: one type of float32, float16, bfloat16, not {q.dtype}, {k.dtype}, {v.dtype}")
-    T, D, kv = step.tokens, step.head_dim, step.kv_heads
-    x.q_stride = _row_stride(q, T, step.heads, D, "q")
-    x.k_stride = _row_stride(k, T, kv, D, "k")
-    x.v_stride = _row_stride(v, T, kv, D, "v")
+    x.q_stride = _row_stride(q, step._q_like, "q")
+    x.k_stride = _row_stride(k, step._kv_like, "k")
+    x.v_stride = _row_stride(v, step._kv_like, "v")
     x.q, x.k, x.v, x.x_dtype = q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtypes[dtype]
     if out is None:
-        out = torch.empty((T, step.heads, D), dtype=step.dtype, device=q.device)
-    elif out.dtype != step.dtype or not out.is_contiguous() or out.numel() != T * step.heads * D:
-        raise ValueError(f"out: a contiguous {step.dtype} tensor [{T}, {step.heads}, {D}]")
+        out = torch.empty_like(step._q_of, memory_format=torch.contiguous_format)
+    elif out.dtype != step.dtype or not out.is_contiguous() or out.numel() != step._q_of.numel():
+        raise ValueError(f"out: a contiguous {step.dtype} tensor {list(step._q_like[0])}")
     rc = B._call(_entry["spqr_cache_store"], step.desc, layer, step._rows_at, out, _stream_ptr(stream))
     if rc != 0:
         _check(rc, "spqr_cache_store")
@@ -216,16 +230,15 @@ def spqr_tree_attention(step: SpQRStep, q, layer: int = 0, out=None, stream=None
     the new ones that their masks show; out has q's shape (rows that belong to no request are left as they are)."""
     if q.dtype != step.dtype:
         raise ValueError(f"q: {step.dtype}, not {q.dtype}")
-    T, H, D = step.tokens, step.heads, step.head_dim
-    q_stride = _row_stride(q, T, H, D, "q")
+    q_stride = _row_stride(q, step._q_like, "q")
     if out is None:
         import torch
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
-        out_stride = H * D
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+        out_stride = step._q_like[1][0]
     else:
         if out.dtype != step.dtype:
             raise ValueError(f"out: {step.dtype}, not {out.dtype}")
-        out_stride = _row_stride(out, T, H, D, "out")
+        out_stride = _row_stride(out, step._q_like, "out")
     rc = B._call(_entry["spqr_tree_attention"], step.desc, layer, q, q_stride, out, out_stride, _stream_ptr(stream))
     if rc != 0:
         _check(rc, "spqr_tree_attention")
