@@ -52,7 +52,8 @@ struct AttendPlan {              // of a launch; host
   int join_x, join_y;
 };
 
-// D = 64, 96, 128, 256; T = _Float16, __bf16.  a.chunk_rows: 16, 32, 48 or 64 (D = 256: 32 at most).
+// D = 64, 96, 128, 256; T = _Float16, __bf16.  a.chunk_rows: 16, 32, 64 (not with D = 256), or what four
+// wavefronts have with rows of their own: 256 (D = 256: 128).
 template <typename T, int D> hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st);
 
 constexpr int kTile = 32;        // keys
@@ -209,18 +210,23 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return r;
 }
 
-template <typename T, int D, int MT>
+// MT: 16-row tiles of a wavefront.  KW = 4: the four wavefronts take every fourth tile of keys for the same rows.  KW = 1: each has
+// rows of its own, for many rows over the same keys, which come out of the caches three times in four; nothing to add up.
+template <typename T, int D, int MT, int KW>
 __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   constexpr int DC = D / 32;                 // 32-element pieces of a key
   constexpr int E = D / 16, EW = E / 2;      // elements and dwords of a value that a lane loads
-  constexpr int kRows = 16 * MT;
-  constexpr int kParts = 4 / MT;             // wavefronts that share 16 rows' results at the end
+  constexpr int kTiles = MT * 4 / KW, kRows = 16 * kTiles;
+  constexpr int kParts = KW == 4 ? 4 / MT : 1;                 // wavefronts that share 16 rows' results at the end
   extern __shared__ __align__(16) Request requests[];        // [requests], then the ends of their parts of the line
   __shared__ int64_t wave_sums[4];
-  __shared__ float so[4][MT][E][kParts][64][4 / kParts];
-  __shared__ float sm[4][kRows], sl[4][kRows];
+  constexpr int kMeet = 4 * MT * E * 256, kQueries = kTiles * DC * 256;        // floats
+  __shared__ __align__(16) float shared[KW == 4 && kMeet > kQueries ? kMeet : kQueries];
+  float(*so)[MT][E][kParts][64][4 / kParts] = reinterpret_cast<float(*)[MT][E][kParts][64][4 / kParts]>(shared);      // [4]
+  __shared__ float sm[4][KW == 4 ? kRows : 1], sl[4][KW == 4 ? kRows : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), x16 = lane & 15, g = lane >> 4;
+  const int key_wave = KW == 4 ? wave : 0, m0 = KW == 4 ? 0 : wave * MT;      // m0: the first of this wavefront's 16-row tiles
   int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
   if (tid == 0) a.joins[blockIdx.x].parts = 0;
   const int64_t line = lay_line(a, line_ends, requests, wave_sums);
@@ -259,8 +265,8 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
 
   // Queries stay in registers where one wavefront's are few, else in LDS, where all four read them: in the place of what the
   // results meet in later.
-  constexpr bool kShared = MT > 1;
-  u32x4(*shared_q)[DC][64] = reinterpret_cast<u32x4(*)[DC][64]>(&so[0][0][0][0][0][0]);
+  constexpr bool kShared = kTiles > 1;
+  u32x4(*shared_q)[DC][64] = reinterpret_cast<u32x4(*)[DC][64]>(shared);
   u32x4 q[kShared ? 1 : MT][DC];
   // A wavefront that is alone on its SIMD has the keys and values of its next two tiles on their way, else of one.
   constexpr int kAhead = MT > 1 && MT * D <= 384 ? 2 : 1;
@@ -301,7 +307,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     table = (const SPQR_SCALAR int32_t*)(a.table + (int64_t)x.r * a.max_pages);
     kh = static_cast<const T*>(a.k) + (int64_t)x.h * page * D;
     vh = static_cast<const T*>(a.v) + (int64_t)x.h * page * D;
-    if (x.t0 + wave < x.t1) load_tile(x.t0 + wave);
+    if (x.t0 + key_wave < x.t1) load_tile(x.t0 + key_wave);
     auto query = [&](int m, int c) {         // (rows that are none: the last one, without a branch, taken as 0)
       const int row = x.row0 + min(16 * m + x16, x.live_rows - 1), tok = token_of(a, row);
       const T* from = static_cast<const T*>(a.q) + (int64_t)(x.rq.first_row + tok) * a.q_stride + (x.h * a.group + row - tok * a.group) * D + 8 * g;
@@ -309,13 +315,13 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       return 16 * m + x16 < x.live_rows ? v ^ a.turn : u32x4{0, 0, 0, 0};
     };
 #pragma unroll
-    for (int m = 0; m < MT; ++m) token[m] = 16 * m + x16 < x.live_rows ? token_of(a, x.row0 + 16 * m + x16) : -1;
+    for (int m = 0; m < MT; ++m) token[m] = 16 * (m0 + m) + x16 < x.live_rows ? token_of(a, x.row0 + 16 * (m0 + m) + x16) : -1;
     if constexpr (kShared) {
       __syncthreads();
 #pragma unroll
-      for (int f = 0; f < (MT * DC + 3) / 4; ++f) {
+      for (int f = 0; f < (kTiles * DC + 3) / 4; ++f) {
         const int m = (4 * f + wave) / DC, c = (4 * f + wave) % DC;
-        if (m < MT) shared_q[m][c][lane] = query(m, c);
+        if (m < kTiles) shared_q[m][c][lane] = query(m, c);
       }
       __syncthreads();
     } else {
@@ -355,7 +361,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       for (int m = 0; m < MT; ++m) {
         u32x4 query[DC];
 #pragma unroll
-        for (int c = 0; c < DC; ++c) query[c] = kShared ? shared_q[m][c][lane] : q[kShared ? 0 : m][c];
+        for (int c = 0; c < DC; ++c) query[c] = kShared ? shared_q[m0 + m][c][lane] : q[kShared ? 0 : m][c];
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
           s[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -425,22 +431,22 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     // behind the last tile they are made all the same, without a branch (behind which the compiler would wait), but of one
     // line.
     const int plain_end = min(t1, min(rq.cached, rq.keys) / kTile);
-    int t = now.t0 + wave;
+    int t = 16 * m0 < live_rows ? now.t0 + key_wave : t1;      // (a wavefront whose rows are none)
     if (t < plain_end) {
       const int last = t1 - 1;
       int ids[kAhead + 2][2];                // page ids are on their way for a tile more; [0]: this tile's
       ids[0][0] = id0;
       ids[0][1] = id1;
 #pragma unroll
-      for (int i = 1; i < kAhead + 2; ++i) page_ids(min(t + 4 * i, last), ids[i][0], ids[i][1]);
+      for (int i = 1; i < kAhead + 2; ++i) page_ids(min(t + KW * i, last), ids[i][0], ids[i][1]);
       if constexpr (kAhead == 2) {
-        load_keys(1, min(t + 4, last), ids[1][0], ids[1][1], t + 4 < t1 ? k_lane : 0);
-        load_values(1, min(t + 4, last), ids[1][0], ids[1][1], t + 4 < t1 ? v_lane : 0);
+        load_keys(1, min(t + KW, last), ids[1][0], ids[1][1], t + KW < t1 ? k_lane : 0);
+        load_values(1, min(t + KW, last), ids[1][0], ids[1][1], t + KW < t1 ? v_lane : 0);
       }
       auto step = [&](int b) {               // false: the tile is for the other loop
         if (!(t < plain_end && there(ids[0][0]) && there(ids[0][1]))) return false;
-        const bool more = t + 4 * kAhead < t1;
-        const int following = min(t + 4 * kAhead, last);
+        const bool more = t + KW * kAhead < t1;
+        const int following = min(t + KW * kAhead, last);
         scores(b);
         __builtin_amdgcn_sched_barrier(0);
         load_keys(b, following, ids[kAhead][0], ids[kAhead][1], more ? k_lane : 0);
@@ -452,13 +458,13 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         __builtin_amdgcn_sched_barrier(0);
         load_values(b, following, ids[kAhead][0], ids[kAhead][1], more ? v_lane : 0);
         outputs();
-        t += 4;
+        t += KW;
 #pragma unroll
         for (int i = 0; i <= kAhead; ++i) {
           ids[i][0] = ids[i + 1][0];
           ids[i][1] = ids[i + 1][1];
         }
-        page_ids(min(t + 4 * (kAhead + 1), last), ids[kAhead + 1][0], ids[kAhead + 1][1]);
+        page_ids(min(t + KW * (kAhead + 1), last), ids[kAhead + 1][0], ids[kAhead + 1][1]);
         return true;
       };
       bool odd = false;
@@ -572,7 +578,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int n = 0; n < E; ++n) output(m, n);
-      t += 4;
+      t += KW;
       if (t < t1) load_tile(t);
     }
 
@@ -582,63 +588,84 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     work = next_segment(now);
     if (kEarly && work) open(now);
 
-    // The wavefronts add up in LDS: each takes a 16-row tile, or as many of its elements as kParts leave it: those that a lane
-    // holds in i = i0 .. of a result, E neighbouring elements an i.
-    constexpr int kI = 4 / kParts;
-    const int tile = wave % MT, i0 = wave / MT * kI;
     const bool whole = done.t0 == 0 && done.t1 == done.tiles;
     const int64_t slot = 2 * (int64_t)blockIdx.x + (begin >= done.line ? 0 : 1);
-    __syncthreads();
-#pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      const int row = 16 * m + x16;
-      float l = sum[m];
-      l += __shfl_xor(l, 16);
-      l += __shfl_xor(l, 32);
-      if (g == 0) { sm[wave][row] = top[m]; sl[wave][row] = l; }
-      if (row < live_rows) {
-#pragma unroll
-        for (int n = 0; n < E; ++n)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) so[wave][m][n][i / kI][lane][i % kI] = o[m][n][i];
-      }
-    }
-    __syncthreads();
-    const int in_chunk = 16 * tile + x16;
-    if (wave / MT < kParts && in_chunk < live_rows) {
-      const float best = fmaxf(fmaxf(sm[0][in_chunk], sm[1][in_chunk]), fmaxf(sm[2][in_chunk], sm[3][in_chunk]));
-      float y[kI][E], all = 0.f;
-#pragma unroll
-      for (int k = 0; k < kI; ++k)
-#pragma unroll
-        for (int n = 0; n < E; ++n) y[k][n] = 0.f;
-#pragma unroll
-      for (int w = 0; w < 4; ++w) {
-        const float c = sm[w][in_chunk] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][in_chunk] - best);
-        all = fmaf(c, sl[w][in_chunk], all);
-#pragma unroll
-        for (int n = 0; n < E; ++n)
-#pragma unroll
-          for (int k = 0; k < kI; ++k) y[k][n] = fmaf(c, so[w][tile][n][wave / MT][lane][k], y[k][n]);
-      }
-      const int d = E * (4 * g + i0);
+    // E elements from d on of a row of the chunk, whose sum is `all`
+    auto put = [&](int in_chunk, int d, float* y, float all) {
       if (whole) {
         const int row = done.row0 + in_chunk, tok = token_of(a, row);
-        const float c = 1.f / all;
-        T* to = static_cast<T*>(a.out) + (int64_t)(done.rq.first_row + tok) * a.out_stride + (done.h * a.group + row - tok * a.group) * D + d;
+        const float c = all == 0.f ? 0.f : 1.f / all;
 #pragma unroll
-        for (int k = 0; k < kI; ++k) {
-#pragma unroll
-          for (int n = 0; n < E; ++n) y[k][n] = all == 0.f ? 0.f : y[k][n] * c;
-          store_run<T, E>(to + E * k, y[k]);
-        }
+        for (int n = 0; n < E; ++n) y[n] = all == 0.f ? 0.f : y[n] * c;
+        store_run<T, E>(static_cast<T*>(a.out) + (int64_t)(done.rq.first_row + tok) * a.out_stride + (done.h * a.group + row - tok * a.group) * D + d, y);
       } else {
         float* to = a.part_o + (slot * kRows + in_chunk) * D + d;
 #pragma unroll
+        for (int n = 0; n < E; n += 2) *reinterpret_cast<float2*>(to + n) = make_float2(y[n], y[n + 1]);
+      }
+    };
+    auto put_sums = [&](int in_chunk, float reference, float all) {
+      if (!whole) *reinterpret_cast<float2*>(a.part_ml + 2 * (slot * kRows + in_chunk)) = make_float2(reference, all);
+    };
+    if constexpr (KW == 1) {
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int row = 16 * (m0 + m) + x16;
+        float l = sum[m];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (row < live_rows) {
+          if (g == 0) put_sums(row, top[m], l);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) {
+            float y[E];
+#pragma unroll
+            for (int n = 0; n < E; ++n) y[n] = o[m][n][i];
+            put(row, E * (4 * g + i), y, l);
+          }
+        }
+      }
+    } else {
+      // The wavefronts add up in LDS: each takes a 16-row tile, or as many of its elements as kParts leave it: those that a lane
+      // holds in i = i0 .. of a result, E neighbouring elements an i.
+      constexpr int kI = 4 / kParts;
+      const int tile = wave % MT, i0 = wave / MT * kI;
+      __syncthreads();
+#pragma unroll
+      for (int m = 0; m < MT; ++m) {
+        const int row = 16 * m + x16;
+        float l = sum[m];
+        l += __shfl_xor(l, 16);
+        l += __shfl_xor(l, 32);
+        if (g == 0) { sm[wave][row] = top[m]; sl[wave][row] = l; }
+        if (row < live_rows) {
+#pragma unroll
+          for (int n = 0; n < E; ++n)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) so[wave][m][n][i / kI][lane][i % kI] = o[m][n][i];
+        }
+      }
+      __syncthreads();
+      const int in_chunk = 16 * tile + x16;
+      if (wave / MT < kParts && in_chunk < live_rows) {
+        const float best = fmaxf(fmaxf(sm[0][in_chunk], sm[1][in_chunk]), fmaxf(sm[2][in_chunk], sm[3][in_chunk]));
+        float y[kI][E], all = 0.f;
+#pragma unroll
         for (int k = 0; k < kI; ++k)
 #pragma unroll
-          for (int n = 0; n < E; n += 2) *reinterpret_cast<float2*>(to + E * k + n) = make_float2(y[k][n], y[k][n + 1]);
-        if (i0 == 0 && g == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * (slot * kRows + in_chunk)) = make_float2(best, all);
+          for (int n = 0; n < E; ++n) y[k][n] = 0.f;
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+          const float c = sm[w][in_chunk] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(sm[w][in_chunk] - best);
+          all = fmaf(c, sl[w][in_chunk], all);
+#pragma unroll
+          for (int n = 0; n < E; ++n)
+#pragma unroll
+            for (int k = 0; k < kI; ++k) y[k][n] = fmaf(c, so[w][tile][n][wave / MT][lane][k], y[k][n]);
+        }
+#pragma unroll
+        for (int k = 0; k < kI; ++k) put(in_chunk, E * (4 * g + i0 + k), y[k], all);
+        if (i0 == 0 && g == 0) put_sums(in_chunk, best, all);
       }
     }
     if (tid == 0 && done.t0 == 0 && !whole) {  // the first part of what the cut behind this workgroup divides
@@ -655,20 +682,19 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   }
 }
 
-// Adds the parts of what the cuts divided, in their order, and writes the rows out.  Workgroup x takes the cut behind workgroup x of
-// the attention, a wavefront a row: most cuts divide something.  Where there are few chunks, each of them in many parts
-// (by_chunk), it takes the x-th chunk, and its wavefronts every fourth part of a row.
+// Adds the parts of what the cuts divided, in their order, and writes the rows out.  kLanes lanes have a row's elements: a quarter
+// of a wavefront, so that it takes four rows at once.
+// by_chunk = false: workgroup x takes the cut behind workgroup x of the attention, 16 rows at a time.  true, where there are few
+// chunks, each of them in many parts: the x-th chunk, four rows at a time, its wavefronts every fourth part.
 template <typename T, int D, bool by_chunk>
 __global__ void __launch_bounds__(256) join_kernel(Attend a) {
-  constexpr int PE = D >= 128 ? D / 64 : D == 96 ? 2 : 1;      // elements a lane
-  __shared__ float meet[4][D + 2];
+  constexpr int kLanes = 16, E = D / kLanes;
+  __shared__ float meet[by_chunk ? 3 : 1][4][D + 2];
   __shared__ int64_t wave_sums[4];
   extern __shared__ __align__(16) Request requests[];
-  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6);
-  const int d = min(lane * PE, D - PE);      // (D = 96: the last lanes repeat the last elements)
-  int from = blockIdx.x;
+  const int lane = threadIdx.x & 63, wave = uniform((int)threadIdx.x >> 6), of_row = lane & 15, quarter = lane >> 4, d = of_row * E;
+  int from = blockIdx.x, r = 0;
   int64_t part = 0, at = 0;
-  int r = 0;
   int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
   if constexpr (by_chunk) {
     part = part_size(a, lay_line(a, line_ends, requests, wave_sums));
@@ -677,89 +703,92 @@ __global__ void __launch_bounds__(256) join_kernel(Attend a) {
   for (;;) {
     if constexpr (by_chunk) {
       int64_t chunks;
-      while (r < a.requests && at >= (chunks = (int64_t)chunks_of(a, requests[r]) * a.kv_heads)) { at -= chunks; ++r; }
+      while (r < a.requests && at >= (chunks = uniform((int64_t)chunks_of(a, requests[r]) * a.kv_heads))) { at -= chunks; ++r; }
       if (r >= a.requests) return;
       const int tiles = tiles_of(requests[r]);
-      const int64_t first = (r == 0 ? 0 : line_ends[r - 1]) + at * (tiles + a.start) + a.start;
+      const int64_t first = uniform((r == 0 ? 0 : line_ends[r - 1]) + at * (tiles + a.start) + a.start);
       at += gridDim.x;
-      from = (int)part_of(uniform(first), part);
+      from = (int)part_of(first, part);
       if (part_of(uniform(first + tiles - 1), part) == from) continue;     // whole
     }
     const Join j = a.joins[from];
     if (j.parts == 0) return;
-    const int parts_step = by_chunk ? 4 : 1, part0 = by_chunk ? wave : 0;
-    for (int row = by_chunk ? (int)blockIdx.y : 4 * (int)blockIdx.y + wave; row < j.live_rows; row += by_chunk ? (int)gridDim.y : 4 * (int)gridDim.y) {
+    constexpr int kStep = by_chunk ? 4 : 1;
+    const int part0 = by_chunk ? wave : 0;
+    for (int row0 = by_chunk ? 4 * (int)blockIdx.y : 4 * (4 * (int)blockIdx.y + wave); row0 < j.live_rows; row0 += (by_chunk ? 4 : 16) * (int)gridDim.y) {
+      const int row = min(row0 + quarter, j.live_rows - 1);
       // the parts behind the first lie in the first slots of the next workgroups
       auto place = [&](int i) { return (int64_t)(i == 0 ? j.slot : 2 * (from + i)) * a.chunk_rows + row; };
-      float best = -INFINITY, all = 0.f, y[PE];
+      float best = -INFINITY, all = 0.f, y[E];
 #pragma unroll
-      for (int e = 0; e < PE; ++e) y[e] = 0.f;
-      for (int i0 = part0; i0 < j.parts; i0 += 64 * parts_step) {
-        const int own = i0 + lane * parts_step;
-        const float2 ml = own < j.parts ? *reinterpret_cast<const float2*>(a.part_ml + 2 * place(own)) : make_float2(-INFINITY, 0.f);
+      for (int e = 0; e < E; ++e) y[e] = 0.f;
+      for (int i0 = part0; i0 < j.parts; i0 += 16 * kStep) {
+        const int mine = i0 + of_row * kStep;
+        const float2 ml = mine < j.parts ? *reinterpret_cast<const float2*>(a.part_ml + 2 * place(mine)) : make_float2(-INFINITY, 0.f);
         float most = ml.x;
-        for (int k = 32; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
+        for (int k = 8; k > 0; k >>= 1) most = fmaxf(most, __shfl_xor(most, k));
         const float top = fmaxf(best, most);
         const float c = ml.x == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(ml.x - top), back = best == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(best - top);
         float l = c * ml.y;
-        for (int k = 32; k > 0; k >>= 1) l += __shfl_xor(l, k);
+        for (int k = 8; k > 0; k >>= 1) l += __shfl_xor(l, k);
         all = all * back + l;
         best = top;
 #pragma unroll
-        for (int e = 0; e < PE; ++e) y[e] *= back;
-        const int n = min(64, (j.parts - i0 + parts_step - 1) / parts_step);
-#pragma unroll 16
+        for (int e = 0; e < E; ++e) y[e] *= back;
+        const int n = min(16, (j.parts - i0 + kStep - 1) / kStep);
+#pragma unroll 8
         for (int i = 0; i < n; ++i) {
-          const float w = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, c), i));
-          float v[PE];
-          __builtin_memcpy(v, __builtin_assume_aligned(a.part_o + place(i0 + i * parts_step) * D + d, 4 * PE), 4 * PE);
+          const float w = __shfl(c, 16 * quarter + i);
+          float v[E];
+          __builtin_memcpy(v, __builtin_assume_aligned(a.part_o + place(i0 + i * kStep) * D + d, E % 4 == 0 ? 16 : 8), 4 * E);
 #pragma unroll
-          for (int e = 0; e < PE; ++e) y[e] = fmaf(w, v[e], y[e]);
+          for (int e = 0; e < E; ++e) y[e] = fmaf(w, v[e], y[e]);
         }
       }
       if constexpr (by_chunk) {
         __syncthreads();
+        if (wave != 0) {
 #pragma unroll
-        for (int e = 0; e < PE; ++e) meet[wave][d + e] = y[e];
-        if (lane == 0) { meet[wave][D] = best; meet[wave][D + 1] = all; }
+          for (int e = 0; e < E; ++e) meet[wave - 1][quarter][d + e] = y[e];
+          if (of_row == 0) { meet[wave - 1][quarter][D] = best; meet[wave - 1][quarter][D + 1] = all; }
+        }
         __syncthreads();
         if (wave != 0) continue;
-        best = fmaxf(fmaxf(meet[0][D], meet[1][D]), fmaxf(meet[2][D], meet[3][D]));
-        all = 0.f;
+        for (int w = 0; w < 3; ++w) {
+          const float m = meet[w][quarter][D], top = fmaxf(best, m);
+          const float c = m == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(m - top), back = best == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(best - top);
+          all = all * back + c * meet[w][quarter][D + 1];
 #pragma unroll
-        for (int e = 0; e < PE; ++e) y[e] = 0.f;
-        for (int w = 0; w < 4; ++w) {
-          const float c = meet[w][D] == -INFINITY ? 0.f : __builtin_amdgcn_exp2f(meet[w][D] - best);
-          all = fmaf(c, meet[w][D + 1], all);
-#pragma unroll
-          for (int e = 0; e < PE; ++e) y[e] = fmaf(c, meet[w][d + e], y[e]);
+          for (int e = 0; e < E; ++e) y[e] = y[e] * back + c * meet[w][quarter][d + e];
+          best = top;
         }
       }
+      if (row0 + quarter >= j.live_rows) continue;
       const float c = 1.f / all;
-      const int full = j.row0 + row, tok = token_of(a, full);
-      T out[PE];
 #pragma unroll
-      for (int e = 0; e < PE; ++e) out[e] = (T)(all == 0.f ? 0.f : y[e] * c);
-      T* to = static_cast<T*>(a.out) + (int64_t)(j.first_row + tok) * a.out_stride + (j.h * a.group + full - tok * a.group) * D + d;
-      __builtin_memcpy(__builtin_assume_aligned(to, 2 * PE), out, 2 * PE);
+      for (int e = 0; e < E; ++e) y[e] = all == 0.f ? 0.f : y[e] * c;
+      const int full = j.row0 + row, tok = token_of(a, full);
+      store_run<T, E>(static_cast<T*>(a.out) + (int64_t)(j.first_row + tok) * a.out_stride + (j.h * a.group + full - tok * a.group) * D + d, y);
     }
     if constexpr (!by_chunk) return;
   }
 }
 
-template <typename T, int D, int MT>
+template <typename T, int D, int MT, int KW>
 static hipError_t launch_chunks(const Attend& a, const AttendPlan& p, hipStream_t st) {
   const size_t lds = (size_t)a.requests * (sizeof(int64_t) + sizeof(Request));
-  hipLaunchKernelGGL((attend_kernel<T, D, MT>), dim3(p.workgroups), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, MT, KW>), dim3(p.workgroups), dim3(256), lds, st, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st) {
+  constexpr int kWide = D == 256 ? 2 : 4;
   hipError_t e = hipErrorInvalidValue;
-  if (a.chunk_rows == 16) e = launch_chunks<T, D, 1>(a, p, st);
-  else if (a.chunk_rows == 32) e = launch_chunks<T, D, 2>(a, p, st);
-  else if constexpr (D < 256) e = a.chunk_rows == 48 ? launch_chunks<T, D, 3>(a, p, st) : launch_chunks<T, D, 4>(a, p, st);
+  if (a.chunk_rows == 16) e = launch_chunks<T, D, 1, 4>(a, p, st);
+  else if (a.chunk_rows == 32) e = launch_chunks<T, D, 2, 4>(a, p, st);
+  else if (a.chunk_rows == 64 * kWide) e = launch_chunks<T, D, kWide, 1>(a, p, st);
+  else if constexpr (D < 256) e = launch_chunks<T, D, 4, 4>(a, p, st);
   if (e != hipSuccess) return e;
   const size_t lds = (size_t)a.requests * (sizeof(int64_t) + sizeof(Request));
   if (p.by_chunk) hipLaunchKernelGGL((join_kernel<T, D, true>), dim3(p.join_x, p.join_y), dim3(256), lds, st, a);

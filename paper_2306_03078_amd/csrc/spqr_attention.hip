@@ -16,8 +16,9 @@ SPQR_ATTEND_EXTERN(256)
 static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   AttendPlan p;
   const int64_t rows = (int64_t)(s->max_fresh > 0 ? s->max_fresh : SPQR_MAX_FRESH) * (s->heads / s->kv_heads);
-  const int most = s->head_dim == 256 ? 32 : 64;
-  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 || most == 32 ? 32 : rows <= 64 ? 64 : 48;
+  const int most = s->head_dim == 256 ? 32 : 64;           // rows that one wavefront has registers for
+  const int64_t kv_bytes = 4ll * s->requests * s->kv_heads * s->head_dim * min((int64_t)s->max_pages * s->page, (int64_t)s->pages * s->page);
+  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || kv_bytes < (64 << 20) ? most : 4 * most;
   a->start = a->chunk_rows == 16 ? 4 : a->chunk_rows == 32 ? 8 : 16;
   // as many as run at once: two of four wavefronts a CU with 16 rows (one with D = 256), else one
   p.workgroups = a->chunk_rows == 16 && s->head_dim < 256 ? 512 : 256;
@@ -25,7 +26,7 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   const int64_t chunks = (int64_t)s->requests * s->kv_heads * ((rows + a->chunk_rows - 1) / a->chunk_rows);
   p.by_chunk = chunks * 16 < p.workgroups;
   p.join_x = p.by_chunk ? (int)chunks : p.workgroups;
-  p.join_y = (int)(p.by_chunk ? live : (live + 3) / 4);
+  p.join_y = (int)((live + (p.by_chunk ? 3 : 15)) / (p.by_chunk ? 4 : 16));
   return p;
 }
 
