@@ -311,8 +311,8 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     auto query = [&](int m, int c) {         // (rows that are none: the last one, without a branch, taken as 0)
       const int row = x.row0 + min(16 * m + x16, x.live_rows - 1), tok = token_of(a, row);
       const T* from = static_cast<const T*>(a.q) + (int64_t)(x.rq.first_row + tok) * a.q_stride + (x.h * a.group + row - tok * a.group) * D + 8 * g;
-      const u32x4 v = *reinterpret_cast<const u32x4*>(from + 32 * c);
-      return 16 * m + x16 < x.live_rows ? v ^ a.turn : u32x4{0, 0, 0, 0};
+      const uint32_t live = 16 * m + x16 < x.live_rows ? ~0u : 0u;
+      return (*reinterpret_cast<const u32x4*>(from + 32 * c) ^ a.turn) & live;
     };
 #pragma unroll
     for (int m = 0; m < MT; ++m) token[m] = 16 * (m0 + m) + x16 < x.live_rows ? token_of(a, x.row0 + 16 * (m0 + m) + x16) : -1;
