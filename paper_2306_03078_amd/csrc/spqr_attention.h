@@ -43,6 +43,7 @@ struct Attend {
   float inv_group;
   int workgroups;
   int chunk_rows, start;         // of a chunk; places of the line in front of its tiles
+  int whole;                     // 1: a chunk is one place, nothing is cut
   double inv_workgroups;
 };
 
@@ -129,7 +130,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Requ
     if (r >= a.requests) break;
     const Request x = request_of(a, r);
     requests[r] = x;
-    ends[r] = sum += x.rows == 0 ? 0 : (int64_t)(tiles_of(x) + a.start) * chunks_of(a, x) * a.kv_heads;
+    ends[r] = sum += x.rows == 0 ? 0 : (int64_t)(a.whole ? 1 : tiles_of(x) + a.start) * chunks_of(a, x) * a.kv_heads;
   }
   int64_t upto = sum;
   for (int d = 1; d < 64; d <<= 1) {
@@ -155,7 +156,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Requ
 __device__ __forceinline__ int64_t part_size(const Attend& a, int64_t line) {
   int64_t q = uniform((int64_t)((double)line * a.inv_workgroups));
   if (q * a.workgroups < line) ++q;
-  return max((int64_t)kLeast, q);
+  return max((int64_t)(a.whole ? 1 : kLeast), q);
 }
 
 // x / cost, x < cost * 2^24: by the reciprocal, put right.
@@ -228,7 +229,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), x16 = lane & 15, g = lane >> 4;
   const int key_wave = KW == 4 ? wave : 0, m0 = KW == 4 ? 0 : wave * MT;      // m0: the first of this wavefront's 16-row tiles
   int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
-  if (tid == 0) a.joins[blockIdx.x].parts = 0;
+  if (tid == 0 && !a.whole) a.joins[blockIdx.x].parts = 0;
   const int64_t line = lay_line(a, line_ends, requests, wave_sums);
   const int64_t part = part_size(a, line);
   const int64_t begin = blockIdx.x * part, end = min(line, begin + part);
@@ -245,16 +246,16 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       x.rq = {uniform(packed.x), uniform(packed.y), uniform(packed.z), uniform(packed.w)};
       x.r = r;
       x.tiles = tiles_of(x.rq);
-      const int chunks = chunks_of(a, x.rq), cost = x.tiles + a.start;
+      const int chunks = chunks_of(a, x.rq), cost = a.whole ? 1 : x.tiles + a.start;
       const int64_t first = r == 0 ? 0 : uniform(line_ends[r - 1]);
-      const int pair = which_pair(at - first, cost);
+      const int pair = a.whole ? (int)(at - first) : which_pair(at - first, cost);
       x.line = first + (int64_t)pair * cost + a.start;
       x.h = pair / chunks;
       x.row0 = (pair - x.h * chunks) * kRows;
       x.live_rows = min(x.rq.rows * a.group - x.row0, kRows);
-      x.t0 = (int)max(at - x.line, (int64_t)0);
-      x.t1 = (int)min(end - x.line, (int64_t)x.tiles);
-      at = x.line + x.tiles;
+      x.t0 = a.whole ? 0 : (int)max(at - x.line, (int64_t)0);
+      x.t1 = a.whole ? x.tiles : (int)min(end - x.line, (int64_t)x.tiles);
+      at = a.whole ? at + 1 : x.line + x.tiles;
       if (x.t0 < x.t1) return true;
     }
     return false;
@@ -789,7 +790,7 @@ hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st) {
   else if (a.chunk_rows == 32) e = launch_chunks<T, D, 2, 4>(a, p, st);
   else if (a.chunk_rows == 64 * kWide) e = launch_chunks<T, D, kWide, 1>(a, p, st);
   else if constexpr (D < 256) e = launch_chunks<T, D, 4, 4>(a, p, st);
-  if (e != hipSuccess) return e;
+  if (e != hipSuccess || a.whole) return e;
   const size_t lds = (size_t)a.requests * (sizeof(int64_t) + sizeof(Request));
   if (p.by_chunk) hipLaunchKernelGGL((join_kernel<T, D, true>), dim3(p.join_x, p.join_y), dim3(256), lds, st, a);
   else hipLaunchKernelGGL((join_kernel<T, D, false>), dim3(p.join_x, p.join_y), dim3(256), 0, st, a);

@@ -11,6 +11,8 @@ SPQR_ATTEND_EXTERN(96)
 SPQR_ATTEND_EXTERN(128)
 SPQR_ATTEND_EXTERN(256)
 
+constexpr int kWholeTiles = 20;
+
 // Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them.  The hint
 // only chooses; any rows are right with any chunks.
 static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
@@ -22,6 +24,8 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   a->start = a->chunk_rows == 16 ? 4 : a->chunk_rows == 32 ? 8 : 16;
   // as many as run at once: two of four wavefronts a CU with 16 rows (one with D = 256), else one
   p.workgroups = a->chunk_rows == 16 && s->head_dim < 256 ? 512 : 256;
+  // Short prefixes, by the table's width: a second launch takes longer than a chunk's tiles one after the other.
+  a->whole = (int64_t)s->max_pages * s->page <= kWholeTiles * kTile;
   const int64_t live = min(rows, (int64_t)a->chunk_rows);
   const int64_t chunks = (int64_t)s->requests * s->kv_heads * ((rows + a->chunk_rows - 1) / a->chunk_rows);
   p.by_chunk = chunks * 16 < p.workgroups;
