@@ -22,8 +22,8 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   const int64_t kv_bytes = 4ll * s->requests * s->kv_heads * s->head_dim * min((int64_t)s->max_pages * s->page, (int64_t)s->pages * s->page);
   a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || kv_bytes < (64 << 20) ? most : 4 * most;
   a->start = a->chunk_rows == 16 ? 4 : a->chunk_rows == 32 ? 8 : 16;
-  // as many as run at once: two of four wavefronts a CU with 16 rows (one with D = 256), else one
-  p.workgroups = a->chunk_rows == 16 && s->head_dim < 256 ? 512 : 256;
+  // as many as run at once: with 16 rows two or (D = 64) three of four wavefronts a CU, else and with D = 256 one
+  p.workgroups = a->chunk_rows > 16 || s->head_dim == 256 ? 256 : s->head_dim == 64 ? 768 : 512;
   // Short prefixes, by the table's width: a second launch takes longer than a chunk's tiles one after the other.
   a->whole = (int64_t)s->max_pages * s->page <= kWholeTiles * kTile;
   const int64_t live = min(rows, (int64_t)a->chunk_rows);
