@@ -21,7 +21,10 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   const int most = s->head_dim == 256 ? 32 : 64;           // rows that one wavefront has registers for
   const int64_t kv_bytes = 4ll * s->requests * s->kv_heads * s->head_dim * min((int64_t)s->max_pages * s->page, (int64_t)s->pages * s->page);
   a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || kv_bytes < (64 << 20) ? most : 4 * most;
-  a->start = a->chunk_rows == 16 ? 4 : a->chunk_rows == 32 ? 8 : 16;
+  // What a (key head, chunk) costs beside its tiles, in tiles.  Measured with 4 / 8 / 16 / 24 (16 rows: 52 heads of 16 requests of up
+  // to 8192 keys 238 / 222 / 226 / 229 us, 32 heads of 64 elements, 64 requests of up to 1500 76 / 67 / 70 / 74 us); with
+  // 8 / 16 / 24 (32 rows: 45.5 / 42.4 / 45.1 us).
+  a->start = a->chunk_rows == 16 ? 8 : 16;
   // as many as run at once: with 16 rows two or (D = 64) three of four wavefronts a CU, else and with D = 256 one
   p.workgroups = a->chunk_rows > 16 || s->head_dim == 256 ? 256 : s->head_dim == 64 ? 768 : 512;
   // Short prefixes, by the table's width: a second launch takes longer than a chunk's tiles one after the other.

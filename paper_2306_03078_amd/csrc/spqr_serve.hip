@@ -31,56 +31,79 @@ __device__ __forceinline__ int64_t wave_sum(int64_t v) {
 }
 
 // One workgroup a request, a thread a new token.  Each workgroup sums over the requests by itself (12 bytes a request out of the
-// L2): one launch, where a scan of its own in front would be two.  Ancestors by doubling: after k rounds a token's row
-// of bits has its 2^k nearest ones, so a chain of 256 takes 8 rounds in LDS.
+// L2): one launch, where a scan of its own in front would be two.  What bounds it are trips to memory one after the other:
+// lengths, then everything that they place (pages, parents) asked for at once, then the stores.  Ancestors by doubling: after
+// k rounds a token's row of bits has its 2^k nearest ones, so a chain of 256 takes 8 rounds in LDS.
 __global__ void __launch_bounds__(256) plan_kernel(spqr_step_t s) {
-  __shared__ int64_t part[4][7];
+  __shared__ int64_t part[4][5];
+  __shared__ int rows_part[4][2];
   __shared__ uint64_t bits[SPQR_MAX_FRESH][4];
   __shared__ int up[SPQR_MAX_FRESH];
   const int r = blockIdx.x, tid = threadIdx.x, R = s.requests, log_page = __ffs(s.page) - 1;
+  const bool last = r == R - 1;
 
-  // rows, pages wanted and pages given back: those of the requests before this one and of all
-  int64_t sum[7] = {0, 0, 0, 0, 0, 0, 0};
+  const Pages p = pages_of(s, r, log_page);
+  const int64_t cached = max(0, s.cached[r]), taken = s.ends[0], given = s.ends[1];
+  // of the requests before this one and (rows, and for the last workgroup the rest) of all: rows, pages wanted, pages given back
+  int rows_before = 0, rows_all = 0;
+  int64_t sum[5] = {0, 0, 0, 0, 0};          // wanted and given back before; of all; pages cut off
   for (int q = tid; q < R; q += 256) {
-    const Pages p = pages_of(s, q, log_page);
-    const int64_t want = max(0, p.need - p.held), back = max(0, p.held - p.need);
-    sum[0] += p.fresh; sum[1] += want; sum[2] += back; sum[3] += p.cut;
-    if (q < r) { sum[4] += p.fresh; sum[5] += want; sum[6] += back; }
+    const Pages x = pages_of(s, q, log_page);
+    const int64_t want = max(0, x.need - x.held), back = max(0, x.held - x.need);
+    rows_all += x.fresh;
+    if (q < r) { rows_before += x.fresh; sum[0] += want; sum[1] += back; }
+    sum[2] += want; sum[3] += back; sum[4] += x.cut;
   }
-  for (int i = 0; i < 7; ++i) {
+  for (int d = 32; d > 0; d >>= 1) {
+    rows_before += __shfl_xor(rows_before, d);
+    rows_all += __shfl_xor(rows_all, d);
+  }
+  const int sums = last ? 5 : 2;
+  for (int i = 0; i < sums; ++i) {
     sum[i] = wave_sum(sum[i]);
     if ((tid & 63) == 0) part[tid >> 6][i] = sum[i];
   }
-  const Pages p = pages_of(s, r, log_page);
-  const int64_t cached = max(0, s.cached[r]);
-  const int64_t taken = s.ends[0], given = s.ends[1];
-  const int64_t P = s.pages, free_pages = min(max((int64_t)0, given - taken), P);
+  if ((tid & 63) == 0) { rows_part[tid >> 6][0] = rows_before; rows_part[tid >> 6][1] = rows_all; }
   __syncthreads();
-  for (int i = 0; i < 7; ++i) sum[i] = part[0][i] + part[1][i] + part[2][i] + part[3][i];
-  const int64_t first = sum[5], first_back = sum[6];
-  const int total = clamp_to(sum[0], s.tokens), base = clamp_to(sum[4], s.tokens);
-  const int rows = min(p.fresh, s.tokens - base);
-  const int want = max(0, p.need - p.held);
-  const int64_t ring_from = (taken % P + P) % P;
+  const int64_t first = part[0][0] + part[1][0] + part[2][0] + part[3][0], first_back = part[0][1] + part[1][1] + part[2][1] + part[3][1];
+  const int base = min(rows_part[0][0] + rows_part[1][0] + rows_part[2][0] + rows_part[3][0], s.tokens);
+  const int total = min(rows_part[0][1] + rows_part[1][1] + rows_part[2][1] + rows_part[3][1], s.tokens);
+  const int rows = min(p.fresh, s.tokens - base), want = max(0, p.need - p.held), back = max(0, p.held - p.need);
+  const int64_t P = s.pages, free_pages = min(max((int64_t)0, given - taken), P);
+  const int64_t ring_from = (uint64_t)taken < 0x100000000ull ? (uint32_t)taken % (uint32_t)P : (taken % P + P) % P;
   int32_t* table = s.table + (int64_t)r * s.max_pages;
 
+  // places of the ring behind ring_from (less than P, as all numbers of free pages are)
+  auto in_ring = [&](int64_t i) { const int64_t at = ring_from + i; return at < P ? at : at - P; };
   // the page at place i of those that the request is to take
-  auto ring_page = [&](int i) { return first + i < free_pages ? s.pool[(ring_from + first + i) % P] : -1; };
-  for (int i = tid; i < want; i += 256) table[p.held + i] = ring_page(i);
+  auto ring_page = [&](int i) { return first + i < free_pages ? s.pool[in_ring(first + i)] : -1; };
+  // the first of each kind of load together, the stores behind them
+  const int64_t key = cached + tid, at = key >> log_page;
+  int id = -1, near = -1, page0 = -1, gone0 = 0;
+  if (tid < rows) {
+    id = at >= s.max_pages ? -1 : at < p.held ? table[at] : ring_page((int)at - p.held);
+    near = s.parent != nullptr ? s.parent[base + tid] : tid - 1;
+  }
+  if (tid < want) page0 = ring_page(tid);
+  if (tid < back) gone0 = table[p.need + tid];
+
+  for (int i = tid; i < want; i += 256) table[p.held + i] = i == tid ? page0 : ring_page(i);
   // behind the ring's end; what would run into its beginning (more free pages than there are) is left out
-  for (int i = tid; i < p.held - p.need; i += 256) {
+  for (int i = tid; i < back; i += 256) {
     const int64_t to = (given - taken) + first_back + i;
-    if (to >= 0 && to < P) s.pool[(ring_from + to) % P] = table[p.need + i];
+    if (to >= 0 && to < P) s.pool[in_ring(to)] = i == tid ? gone0 : table[p.need + i];
   }
   if (tid == 0) {
     s.q_start[r] = base;
     const int64_t granted = min((int64_t)want, max((int64_t)0, free_pages - first));
     s.held_out[r] = p.held > p.need ? p.need : p.held + (int)granted;
-    if (r == R - 1) {
+    if (last) {
+      int64_t all[3];
+      for (int i = 0; i < 3; ++i) all[i] = part[0][i + 2] + part[1][i + 2] + part[2][i + 2] + part[3][i + 2];
       s.q_start[R] = total;
-      s.ends_out[0] = taken + min(sum[1], free_pages);
-      s.ends_out[1] = given + sum[2];
-      s.ends_out[2] = max((int64_t)0, sum[1] - free_pages) + sum[3];
+      s.ends_out[0] = taken + min(all[0], free_pages);
+      s.ends_out[1] = given + all[1];
+      s.ends_out[2] = max((int64_t)0, all[0] - free_pages) + all[2];
     }
   }
 
@@ -92,10 +115,9 @@ __global__ void __launch_bounds__(256) plan_kernel(spqr_step_t s) {
       own[w] = n == 0 ? 0 : ~0ull >> (64 - n);
     }
   } else {                       // every wavefront takes part, also one without rows
-    own[tid >> 6] = 1ull << (tid & 63);
-    for (int w = 0; w < 4; ++w) bits[tid][w] = own[w];
-    int next = tid < rows ? s.parent[base + tid] : -1;
-    up[tid] = next = next >= 0 && next < tid ? next : -1;
+    for (int w = 0; w < 4; ++w) bits[tid][w] = own[w] = w == tid >> 6 ? 1ull << (tid & 63) : 0;
+    int next = near >= 0 && near < tid ? near : -1;
+    up[tid] = next;
     while (__syncthreads_or(next >= 0)) {
       int behind = -1;
       if (next >= 0) {
@@ -109,8 +131,6 @@ __global__ void __launch_bounds__(256) plan_kernel(spqr_step_t s) {
     depth = __popcll(own[0]) + __popcll(own[1]) + __popcll(own[2]) + __popcll(own[3]) - 1;
   }
   if (tid < rows) {
-    const int64_t key = cached + tid, at = key >> log_page;
-    const int id = at >= s.max_pages ? -1 : at < p.held ? table[at] : ring_page((int)at - p.held);
     const int64_t t = base + tid;
     s.slot[t] = id >= 0 && id < P ? (int32_t)((int64_t)id * s.page + (key & (s.page - 1))) : -1;
     s.position[t] = (int32_t)min(cached + depth, (int64_t)0x7FFFFFFF);
