@@ -303,6 +303,57 @@ def test_offsets_beyond_32_bits(S):
         assert torch.equal(p.k[0, s // page, :, s % page], x[t]) and torch.equal(p.v[0, s // page, :, s % page], 2 * x[t])
 
 
+def roomy(p, S, **more):
+    """A step over the same cache and tables in a pool of 70 MB and more, with a table as wide: what many rows over long prefixes
+    take."""
+    import torch
+    pages = max(p.pages, -(-(70 << 20) // (4 * len(p.cached) * p.kv * p.D * p.page)))
+    k, v = (torch.full((1, pages) + tuple(p.k.shape[2:]), math.nan, dtype=p.dtype, device="cuda:0") for _ in range(2))
+    k[:, :p.pages], v[:, :p.pages] = p.k, p.v
+    wide = np.full((len(p.cached), pages), -1)
+    wide[:, :p.table.shape[1]] = p.table
+    p.k, p.v, p.pages, p.table = k, v, pages, wide
+    return p.step(S, **more)
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("cached,fresh,heads,kv,D,kind", [
+    ([700, 0, 129], [20, 40, 1], 8, 2, 128, "tree"),             # rows that end inside a wavefront's, chunks with idle wavefronts
+    ([333], [256], 4, 2, 128, "tree"), ([90, 2000], [33, 2], 16, 2, 64, "any"), ([1000, 31], [30, 65], 12, 4, 96, "chain"),
+    ([500, 7], [70, 18], 8, 2, 256, "tree"), ([3000], [100], 8, 1, 256, "any"), ([0, 64], [64, 70], 71, 1, 64, "tree")])
+def test_many_rows_over_long_prefixes(S, dtype, cached, fresh, heads, kv, D, kind):
+    p = Problem(cached, fresh, heads, kv, D, 16, dtype, kind)
+    p.check(S.spqr_tree_attention(roomy(p, S), p.q))
+
+
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("D", [64, 96, 128, 256])
+@pytest.mark.parametrize("rows", [(15, 1), (16, 1), (3, 7), (31, 1), (32, 1), (11, 3), (8, 8), (64, 1), (13, 5)])
+def test_every_number_of_rows_a_chunk_can_have(S, dtype, D, rows):
+    """1 .. 16, 17 .. 32, 33 .. 64 and 65 rows of a key head, over prefixes that one launch takes and that are cut."""
+    fresh, group = rows
+    for cached in ([100, 3], [1500, 64]):
+        p = Problem(cached, [fresh, 1], 2 * group, 2, D, 32, dtype, "tree", seed=fresh)
+        p.check(S.spqr_tree_attention(p.step(S), p.q))
+
+
+@pytest.mark.parametrize("D", [64, 128, 256])
+def test_pages_missing_and_values_masked_under_many_rows(S, D):
+    """NaN in a sibling's value and missing pages, with rows of their own a wavefront."""
+    import torch
+    p = Problem([200, 90], [70, 40], 4, 2, D, 16, "float16", "tree")
+    p.table[0, 2], p.table[1, 1] = -1, 10 ** 6
+    vis = p.visible(0)
+    j = next(k for k in range(201, 270) if vis[:, k].any() and not vis[:, k].all())
+    want = S.spqr_tree_attention(roomy(p, S), p.q)
+    p.check(want)
+    p.v[0, p.table[0, j // 16], :, j % 16] = math.nan
+    got = S.spqr_tree_attention(p.step(S), p.q)
+    sees = torch.from_numpy(vis[:, j]).cuda()
+    assert torch.equal(got[:70][~sees], want[:70][~sees]) and torch.equal(got[70:], want[70:])
+    assert bool(torch.isnan(got[:70][sees]).all())
+
+
 def test_same_bits_every_time_on_any_stream_and_from_a_graph(S):
     import torch
     p = Problem([900, 20, 333], [16, 1, 9], 16, 4, 128, 16, "bfloat16", "tree")

@@ -130,6 +130,30 @@ def test_attention_refuses():
         assert attend(descriptor(scale=scale)) == PARAM
 
 
+def test_attention_refuses_a_workspace_that_is_none():
+    need = S._lib().spqr_tree_attention_workspace_bytes(C.byref(descriptor()))
+    assert need > 0
+    assert attend(descriptor(workspace=None)) == NULL and attend(descriptor(workspace=SOME + 128)) == ALIGN
+    for size in (0, -1, need - 1):
+        assert attend(descriptor(workspace_bytes=size)) == WORKSPACE
+    assert attend(descriptor(heads=2048, kv_heads=1)) == SHAPE
+
+
+@pytest.mark.parametrize("head_dim", [64, 96, 128, 256])
+def test_the_workspace_goes_by_the_sizes_and_not_by_pointers(head_dim):
+    """As many rows of partial results, twice a workgroup, as a chunk has."""
+    lib = S._lib()
+    got = set()
+    for max_fresh in (1, 5, 9, 16, 17, 40, 256, 0):
+        for max_pages in (1, 9, 1 << 20):
+            d = descriptor(head_dim=head_dim, max_fresh=max_fresh, max_pages=max_pages, pages=1 << 20)
+            n = lib.spqr_tree_attention_workspace_bytes(C.byref(d))
+            e = descriptor(head_dim=head_dim, max_fresh=max_fresh, max_pages=max_pages, pages=1 << 20, k=SOME, v=SOME, cached=None, table=None, mask=None, workspace=None)
+            assert n == lib.spqr_tree_attention_workspace_bytes(C.byref(e))
+            got.add(n)
+    assert 3 <= len(got) <= 5 and min(got) > 0 and max(got) <= 140 << 20
+
+
 def test_keep_refuses():
     for name in ("cached", "table", "q_start", "cached_out", "mask"):
         assert keep(descriptor(**{name: None})) == NULL and keep(descriptor(**{name: SOME + 2})) == ALIGN
