@@ -203,12 +203,10 @@ struct Segment {
   int64_t line;                              // place of its first tile
 };
 
-// max(a, b, c) as the instruction has it.  (fmaxf makes each operand pass through an instruction of its own first, lest it be a
-// signalling NaN; a NaN score makes its row NaN through its sum.)
+// The largest of three, NaN where one is NaN: an instruction.  (fmaxf makes each operand pass through an instruction of its own first,
+// lest it be a signalling NaN.)
 __device__ __forceinline__ float max3(float a, float b, float c) {
-  float r;
-  asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-  return r;
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
 // MT: 16-row tiles of a wavefront.  KW = 4: the four wavefronts take every fourth tile of keys for the same rows.  KW = 1: each has
