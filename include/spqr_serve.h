@@ -112,8 +112,8 @@ int spqr_cache_plan(const spqr_step_t* s, void* stream);
  * with one slot: undefined which stays. */
 int spqr_cache_store(const spqr_step_t* s, int32_t layer, const spqr_rows_t* x, void* q_out, void* stream);
 
-/* Bytes of device scratch that spqr_tree_attention needs for these sizes (requests, tokens, max_fresh, heads, kv_heads,
- * head_dim, dtype); or a negative status.  Host arithmetic only. */
+/* Bytes of device scratch that spqr_tree_attention needs for a step of these sizes; or a negative status.  Host
+ * arithmetic only. */
 int64_t spqr_tree_attention_workspace_bytes(const spqr_step_t* s);
 
 /* out[t][h] = sum_j p_j v_j, p = softmax over the keys j that row t sees of scale * q[t][h] . k_j: all cached tokens of its

@@ -6,8 +6,7 @@
 // O^T = V^T P^T wants: probabilities never leave their lane.  V^T's A operand needs one element of eight keys a lane: a lane
 // loads D / 16 neighbouring elements of the group's eight keys (whole rows, so every line is read once and in order) and
 // exchanges 16-bit halves between its own registers; the n-th instruction then takes the n-th element of each lane.
-// K and V pass through no LDS, a key's bytes are read once for all rows of a chunk (16 * MT rows: tokens times the query
-// heads of one key head).
+// A key's bytes are read once for all rows of a chunk (16 to 256: tokens times the query heads of one key head).
 //
 // The softmax's reference m of a row moves only when a score passes it by 8 (in powers of two; probabilities stay below
 // 2^8): a tile then costs no exchange between lanes.  Sums of probabilities are binary32 and of the unrounded ones, a
@@ -16,6 +15,12 @@
 // Work is a line of tiles (request, key head, chunk of rows, 32 keys) that is cut into equal parts, one a workgroup, wherever
 // the cuts fall: lengths are known on the card only.  What a cut divides goes to the workspace as a partial result
 // and join_kernel adds the parts in their order.
+//
+// What bounds it.  Few rows: memory; 16 requests of up to 8192 keys, 52 heads of 128 elements, reads 1.25 GB in 220 us, 5.7 TB/s
+// (a copy reads and writes 4.7 TB/s); 40 rows over 131067 keys, 8 heads, 537 MB in 108 us, 5.0 TB/s.  Short prefixes: two launches
+// and four trips to memory one after the other (lengths, pages, keys, parts); 1024 keys, 32 heads 15.7 us.  Many rows: issue of
+// the matrix cores' and the softmax's instructions; 4096 rows over 260000 keys 580 us, 940 TFLOP/s; 4 requests of up to 64
+// tokens, 64 heads on 8, up to 32000 keys 138 us, 520 TFLOP/s (chunks in part empty, parts written and joined).
 #ifndef SPQR_ATTENTION_INTERNAL_H_
 #define SPQR_ATTENTION_INTERNAL_H_
 #include <cmath>
@@ -121,8 +126,9 @@ __device__ __forceinline__ int chunks_of(const Attend& a, const Request& x) { re
 // The requests, and inclusive prefix sums of their parts of the line, in LDS; returns the line's length.  A (key head, chunk) has
 // a place for each of its tiles, and a.start in front of them for what it costs beside them.  All 256
 // threads; ends with a barrier.
+template <int kWaves>
 __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Request* requests, int64_t* wave_sums) {
-  const int tid = threadIdx.x, lane = tid & 63, each = (a.requests + 255) / 256;
+  const int tid = threadIdx.x, lane = tid & 63, each = (a.requests + 64 * kWaves - 1) / (64 * kWaves);
   int64_t sum = 0;
 #pragma unroll 1
   for (int i = 0; i < each; ++i) {
@@ -141,7 +147,7 @@ __device__ __forceinline__ int64_t lay_line(const Attend& a, int64_t* ends, Requ
   __syncthreads();
   int64_t before = upto - sum, all = 0;
 #pragma unroll
-  for (int w = 0; w < 4; ++w) {
+  for (int w = 0; w < kWaves; ++w) {
     if (w < tid >> 6) before += wave_sums[w];
     all += wave_sums[w];
   }
@@ -209,18 +215,22 @@ __device__ __forceinline__ float max3(float a, float b, float c) {
   return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
 }
 
-// MT: 16-row tiles of a wavefront.  KW = 4: the four wavefronts take every fourth tile of keys for the same rows.  KW = 1: each has
-// rows of its own, for many rows over the same keys, which come out of the caches three times in four; nothing to add up.
+// MT: 16-row tiles of a wavefront.  KW = 4: four wavefronts take every fourth tile of keys for the same rows, out of the cache into
+// registers.  KW = 1: eight wavefronts have rows of their own, for many rows over the same keys: nothing to add up, and full tiles
+// pass through LDS, loaded once for all.
 template <typename T, int D, int MT, int KW>
-__global__ void __launch_bounds__(256) attend_kernel(Attend a) {
+__global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
+  constexpr int kWaves = KW == 1 ? 8 : 4;
   constexpr int DC = D / 32;                 // 32-element pieces of a key
   constexpr int E = D / 16, EW = E / 2;      // elements and dwords of a value that a lane loads
-  constexpr int kTiles = MT * 4 / KW, kRows = 16 * kTiles;
+  constexpr int kTiles = KW == 1 ? MT * kWaves : MT, kRows = 16 * kTiles;
   constexpr int kParts = KW == 4 ? 4 / MT : 1;                 // wavefronts that share 16 rows' results at the end
   extern __shared__ __align__(16) Request requests[];        // [requests], then the ends of their parts of the line
-  __shared__ int64_t wave_sums[4];
+  __shared__ int64_t wave_sums[kWaves];
   constexpr int kMeet = 4 * MT * E * 256, kQueries = kTiles * DC * 256;        // floats
-  __shared__ __align__(16) float shared[KW == 4 && kMeet > kQueries ? kMeet : kQueries];
+  constexpr int kST = D == 256 ? 1 : 2, kKeyRow = D / 8 + 1;                   // tiles of a stage; 16-byte places of a key in LDS
+  constexpr int kStageK = 32 * kST * kKeyRow, kStageV = 4 * kST * D;           // 16-byte places
+  __shared__ __align__(16) float shared[KW == 1 ? 8 * (kStageK + kStageV) : kMeet > kQueries ? kMeet : kQueries];
   float(*so)[MT][E][kParts][64][4 / kParts] = reinterpret_cast<float(*)[MT][E][kParts][64][4 / kParts]>(shared);      // [4]
   __shared__ float sm[4][KW == 4 ? kRows : 1], sl[4][KW == 4 ? kRows : 1];
 
@@ -228,11 +238,17 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
   const int key_wave = KW == 4 ? wave : 0, m0 = KW == 4 ? 0 : wave * MT;      // m0: the first of this wavefront's 16-row tiles
   int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
   if (tid == 0 && !a.whole) a.joins[blockIdx.x].parts = 0;
-  const int64_t line = lay_line(a, line_ends, requests, wave_sums);
+  const int64_t line = lay_line<kWaves>(a, line_ends, requests, wave_sums);
   const int64_t part = part_size(a, line);
   const int64_t begin = blockIdx.x * part, end = min(line, begin + part);
   if (begin >= end) return;
   const int page = 1 << a.log_page;
+  // The thread as the compiler cannot know it: what is computed from it is computed where it is used, and takes no registers elsewhere.
+  auto thread = [&] {
+    uint32_t id = tid;
+    asm volatile("" : "+v"(id));
+    return id;
+  };
   const int64_t page_elements = (int64_t)a.kv_heads * page * D;
 
   int64_t at = begin;
@@ -264,13 +280,11 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
 
   // Queries stay in registers where one wavefront's are few, else in LDS, where all four read them: in the place of what the
   // results meet in later.
-  constexpr bool kShared = kTiles > 1;
+  constexpr bool kShared = KW == 4 && kTiles > 1;
   u32x4(*shared_q)[DC][64] = reinterpret_cast<u32x4(*)[DC][64]>(shared);
   u32x4 q[kShared ? 1 : MT][DC];
-  // A wavefront that is alone on its SIMD has the keys and values of its next two tiles on their way, else of one.
-  constexpr int kAhead = MT > 1 && MT * D <= 384 ? 2 : 1;
-  u32x4 kf[kAhead][2][DC];
-  uint32_t vf[kAhead][8][EW];
+  u32x4 kf[2][DC];                           // the next tile's, on their way while this one is computed
+  uint32_t vf[8][EW];
   int token[MT], id0 = 0, id1 = 0;
   const uint32_t k_lane = x16 * D + 8 * g, v_lane = 4 * g * D + E * x16;
   const T *kh, *vh;
@@ -279,34 +293,34 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     i0 = table[min((t * kTile) >> a.log_page, a.max_pages - 1)];
     i1 = table[min((t * kTile + 16) >> a.log_page, a.max_pages - 1)];
   };
-  auto load_keys = [&](int b, int t, int i0, int i1, uint32_t from) {
+  auto load_keys = [&](int t, int i0, int i1, uint32_t from) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const T* base = kh + half_offset(u ? i1 : i0, t * kTile + 16 * u);
 #pragma unroll
-      for (int c = 0; c < DC; ++c) kf[b][u][c] = *reinterpret_cast<const u32x4*>(base + (from + 32 * c));
+      for (int c = 0; c < DC; ++c) kf[u][c] = *reinterpret_cast<const u32x4*>(base + (from + 32 * c));
     }
   };
-  auto load_values = [&](int b, int t, int i0, int i1, uint32_t from) {
+  auto load_values = [&](int t, int i0, int i1, uint32_t from) {
 #pragma unroll
     for (int u = 0; u < 2; ++u) {
       const T* base = vh + half_offset(u ? i1 : i0, t * kTile + 16 * u);
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        __builtin_memcpy(vf[b][4 * u + i], __builtin_assume_aligned(base + (from + i * D), E % 8 == 0 ? 16 : E % 4 == 0 ? 8 : 4), 4 * EW);
+        __builtin_memcpy(vf[4 * u + i], __builtin_assume_aligned(base + (from + i * D), E % 8 == 0 ? 16 : E % 4 == 0 ? 8 : 4), 4 * EW);
     }
   };
   auto load_tile = [&](int t) {
     page_ids(t, id0, id1);
-    load_keys(0, t, id0, id1, k_lane);
-    load_values(0, t, id0, id1, v_lane);
+    load_keys(t, id0, id1, k_lane);
+    load_values(t, id0, id1, v_lane);
   };
   // a segment's queries and this wavefront's first tile; a row is (token, query head of the group)
   auto open = [&](const Segment& x) {
     table = (const SPQR_SCALAR int32_t*)(a.table + (int64_t)x.r * a.max_pages);
     kh = static_cast<const T*>(a.k) + (int64_t)x.h * page * D;
     vh = static_cast<const T*>(a.v) + (int64_t)x.h * page * D;
-    if (x.t0 + key_wave < x.t1) load_tile(x.t0 + key_wave);
+    if (KW == 4 && x.t0 + key_wave < x.t1) load_tile(x.t0 + key_wave);
     auto query = [&](int m, int c) {         // (rows that are none: the last one, without a branch, taken as 0)
       const int row = x.row0 + min(16 * m + x16, x.live_rows - 1), tok = token_of(a, row);
       const T* from = static_cast<const T*>(a.q) + (int64_t)(x.rq.first_row + tok) * a.q_stride + (x.h * a.group + row - tok * a.group) * D + 8 * g;
@@ -325,7 +339,9 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
       __syncthreads();
     } else {
 #pragma unroll
-      for (int c = 0; c < DC; ++c) q[0][c] = query(0, c);
+      for (int m = 0; m < MT; ++m)
+#pragma unroll
+        for (int c = 0; c < DC; ++c) q[m][c] = query(m0 + m, c);
     }
   };
 
@@ -351,11 +367,11 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     f32x4 s[MT][2];
     u32x4 vt[E];
     uint32_t p[MT][4], seen[MT];
-    auto transpose = [&](int b, int k) {       // the k-th of 4 E exchanges
+    auto transpose = [&](int k) {       // the k-th of 4 E exchanges
       const int n = k / 4, j = k % 4;
-      vt[n][j] = __builtin_amdgcn_perm(vf[b][2 * j + 1][n / 2], vf[b][2 * j][n / 2], n & 1 ? 0x07060302 : 0x05040100);
+      vt[n][j] = __builtin_amdgcn_perm(vf[2 * j + 1][n / 2], vf[2 * j][n / 2], n & 1 ? 0x07060302 : 0x05040100);
     };
-    auto scores = [&](int b) {
+    auto scores = [&] {
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
         u32x4 query[DC];
@@ -365,11 +381,11 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         for (int u = 0; u < 2; ++u) {
           s[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-          for (int c = 0; c < DC; ++c) s[m][u] = Matrix<T>::product(kf[b][u][c], query[c], s[m][u]);
+          for (int c = 0; c < DC; ++c) s[m][u] = Matrix<T>::product(kf[u][c], query[c], s[m][u]);
         }
       }
     };
-    auto references = [&](auto masked_tile) {  // where scores are too large for a row's reference, a new one
+    auto references = [&](auto masked_tile, int of4) {  // where scores are too large for a row's reference, a new one
       constexpr bool masked = decltype(masked_tile)::value;
       float most[MT];
       bool moves = false;
@@ -378,7 +394,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         if constexpr (masked) {
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (!(seen[m] >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1)) s[m][j >> 2][j & 3] = -INFINITY;
+            if (!(seen[m] >> (16 * (j >> 2) + 4 * of4 + (j & 3)) & 1)) s[m][j >> 2][j & 3] = -INFINITY;
         }
         const f32x4 x = s[m][0], y = s[m][1];
         most[m] = max3(max3(x[0], x[1], x[2]), max3(x[3], y[0], y[1]), max3(y[2], y[3], y[3])) * a.scale2;
@@ -431,66 +447,193 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     // line.
     const int plain_end = min(t1, min(rq.cached, rq.keys) / kTile);
     int t = 16 * m0 < live_rows ? now.t0 + key_wave : t1;      // (a wavefront whose rows are none)
-    if (t < plain_end) {
+    if constexpr (KW == 1) {
+      // A stage of one or two tiles lies in LDS in the order in which the matrix cores take it: keys row by row, each row 16 bytes
+      // longer than it is, so that 16 keys' pieces lie in different banks; of the values the eight keys of a group element by element,
+      // transposed once for all eight wavefronts, the places of neighbouring pairs of elements exchanged (^) so that a thread's two
+      // stores meet no bank twice.  The next stage is on its way through registers: pieces of 16 bytes of the keys, two
+      // elements of eight keys of the values a thread.  A barrier a stage: behind it the last stage's buffer is free and this one's
+      // is full.
+      // Measured against four wavefronts of 64 rows that each load every tile (KW = 4's way): 512 rows, 8 heads of 128 over up to
+      // 32000 keys, 4 requests 151 -> 138 us; 4096 rows over 260000 keys of one head 631 -> 580 us (940 TFLOP/s); heads of 64
+      // elements 60 -> 49 us, of 256 194 -> 154 us.  Dropped: two stages on their way with the queries in LDS (their registers'
+      // place; 162 us), priorities around the products (141 us), halves of the wavefronts half a stage apart (151 us).
+      constexpr int kK = (4 * kST * D + 511) / 512, kV = (2 * kST * D + 511) / 512;
+      u32x4* stage = reinterpret_cast<u32x4*>(shared);                         // [2][kStageK + kStageV]
+      u32x4 k_on_way[kK];
+      uint32_t v_on_way[kV][8];
       const int last = t1 - 1;
-      int ids[kAhead + 2][2];                // page ids are on their way for a tile more; [0]: this tile's
-      ids[0][0] = id0;
-      ids[0][1] = id1;
+      int at_tile = now.t0;
+      // pages of a stage: those of the keys and values that this wavefront loads, and whether all are there
+      int k_id[kK], v_id[kV][2];
+      auto half_id = [&](int half) { return table[min((min(half >> 1, last) * kTile + 16 * (half & 1)) >> a.log_page, a.max_pages - 1)]; };
+      auto stage_ids = [&](int from) {
 #pragma unroll
-      for (int i = 1; i < kAhead + 2; ++i) page_ids(min(t + KW * i, last), ids[i][0], ids[i][1]);
-      if constexpr (kAhead == 2) {
-        load_keys(1, min(t + KW, last), ids[1][0], ids[1][1], t + KW < t1 ? k_lane : 0);
-        load_values(1, min(t + KW, last), ids[1][0], ids[1][1], t + KW < t1 ? v_lane : 0);
+        for (int i = 0; i < kK; ++i) k_id[i] = half_id(2 * from + (64 * wave + 512 * i) / (2 * D));
+#pragma unroll
+        for (int i = 0; i < kV; ++i)
+#pragma unroll
+          for (int u = 0; u < 2; ++u) v_id[i][u] = half_id(2 * (from + (64 * wave + 512 * i) / (2 * D)) + u);
+        bool all = from + kST <= plain_end;
+#pragma unroll
+        for (int i = 0; i < 2 * kST; ++i) all &= there(half_id(2 * from + i));
+        return all;
+      };
+      auto fetch = [&](int from, bool whole_stage) {
+        const uint32_t me = thread();
+#pragma unroll
+        for (int i = 0; i < kK; ++i) {
+          const int first = 64 * wave + 512 * i;
+          if (512 * (i + 1) <= 4 * kST * D || first < 4 * kST * D) {
+            const int half = first / (2 * D);
+            const T* base = kh + half_offset(k_id[i], min(from + half / 2, last) * kTile + 16 * (half & 1));
+            const uint32_t unit = me + 512 * i, key = unit / (D / 8);
+            k_on_way[i] = *reinterpret_cast<const u32x4*>(base + (whole_stage ? (key & 15) * D + 8 * (unit - key * (D / 8)) : 0));
+          }
+        }
+#pragma unroll
+        for (int i = 0; i < kV; ++i) {
+          const int first = 64 * wave + 512 * i;
+          if (512 * (i + 1) <= 2 * kST * D || first < 2 * kST * D) {
+            const int tile = first / (2 * D);
+            const uint32_t unit = me + 512 * i - tile * 2 * D, group = unit / (D / 2);
+            const uint32_t from_lane = whole_stage ? 4 * group * D + 2 * (unit - group * (D / 2)) : 0;
+#pragma unroll
+            for (int u = 0; u < 2; ++u) {
+              const T* base = vh + half_offset(v_id[i][u], min(from + tile, last) * kTile + 16 * u);
+#pragma unroll
+              for (int j = 0; j < 4; ++j) v_on_way[i][4 * u + j] = *reinterpret_cast<const uint32_t*>(base + (from_lane + j * D));
+            }
+          }
+        }
+      };
+      auto lay_down = [&](int b) {
+        const uint32_t me = thread();
+        u32x4* to_k = stage + b * (kStageK + kStageV);
+        u32x4* to_v = to_k + kStageK;
+#pragma unroll
+        for (int i = 0; i < kK; ++i)
+          if (512 * (i + 1) <= 4 * kST * D || 64 * wave + 512 * i < 4 * kST * D) {
+            const uint32_t unit = me + 512 * i, key = unit / (D / 8);
+            to_k[key * kKeyRow + unit - key * (D / 8)] = k_on_way[i];
+          }
+#pragma unroll
+        for (int i = 0; i < kV; ++i)
+          if (512 * (i + 1) <= 2 * kST * D || 64 * wave + 512 * i < 2 * kST * D) {
+            const uint32_t unit = me + 512 * i, group = unit / (D / 2), d = 2 * (unit - group * (D / 2)), n = d % E;
+            u32x4 even, odd;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              even[j] = __builtin_amdgcn_perm(v_on_way[i][2 * j + 1], v_on_way[i][2 * j], 0x05040100);
+              odd[j] = __builtin_amdgcn_perm(v_on_way[i][2 * j + 1], v_on_way[i][2 * j], 0x07060302);
+            }
+            u32x4* to = to_v + (group * E + n) * 16 + ((d / E) ^ (n * (16 / E)));
+            to[0] = even;
+            to[16] = odd;
+          }
+      };
+      auto meet = [&] {
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "workgroup", "local");
+        __builtin_amdgcn_s_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
+      };
+      bool ok0 = stage_ids(at_tile);
+      if (ok0) {
+        fetch(at_tile, true);
+        bool ok1 = stage_ids(at_tile + kST);
+        meet();                                // the last segment's stages are read
+        lay_down(0);
+        fetch(at_tile + kST, ok1);
+        bool ok2 = stage_ids(at_tile + 2 * kST);
+        int b = 0;
+        do {
+          meet();
+          const uint32_t me = thread(), x = me & 15, of = me >> 4 & 3;
+          const u32x4* keys = stage + b * (kStageK + kStageV) + x * kKeyRow + of;
+          const u32x4* values = stage + b * (kStageK + kStageV) + kStageK + of * E * 16;
+          u32x4 key[2][DC];
+          auto read_keys = [&](int i) {
+#pragma unroll
+            for (int u = 0; u < 2; ++u)
+#pragma unroll
+              for (int c = 0; c < DC; ++c) key[u][c] = keys[(32 * i + 16 * u) * kKeyRow + 4 * c];
+          };
+          auto read_values = [&](int i) {
+#pragma unroll
+            for (int n = 0; n < E; ++n) vt[n] = values[(4 * i * E + n) * 16 + (x ^ ((n & ~1) * (16 / E)))];
+          };
+          read_keys(0);
+#pragma unroll
+          for (int i = 0; i < kST; ++i) {
+            __builtin_amdgcn_sched_barrier(0);
+            if (t < t1) {
+#pragma unroll
+              for (int u = 0; u < 2; ++u)
+#pragma unroll
+                for (int m = 0; m < MT; ++m) {
+                  s[m][u] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+                  for (int c = 0; c < DC; ++c) s[m][u] = Matrix<T>::product(key[u][c], q[m][c], s[m][u]);
+                }
+              __builtin_amdgcn_sched_barrier(0);
+              read_values(i);
+              references(std::false_type(), 0);
+#pragma unroll
+              for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) exponentials(m, k);
+#pragma unroll
+              for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < E; ++n) output(m, n);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            if (i + 1 < kST) read_keys(i + 1);
+            if (i == 0) {
+              lay_down(b ^ 1);
+              fetch(at_tile + 2 * kST, ok2);
+              ok0 = ok1;
+              ok1 = ok2;
+              ok2 = stage_ids(at_tile + 3 * kST);
+            }
+          }
+          at_tile += kST;
+          b ^= 1;
+        } while (ok0);
       }
-      auto step = [&](int b) {               // false: the tile is for the other loop
-        if (!(t < plain_end && there(ids[0][0]) && there(ids[0][1]))) return false;
-        const bool more = t + KW * kAhead < t1;
-        const int following = min(t + KW * kAhead, last);
-        scores(b);
+      if (t < t1) t = at_tile;
+      load_tile(min(t, t1 - 1));             // (also where there is none: then no registers keep the last segment's)
+    } else if (t < plain_end) {
+      const int last = t1 - 1;
+      int next0, next1, then0, then1;        // page ids of the next tile and, on their way, of the one behind it
+      page_ids(min(t + KW, last), next0, next1);
+      page_ids(min(t + 2 * KW, last), then0, then1);
+      while (t < plain_end && there(id0) && there(id1)) {
+        const bool more = t + KW < t1;
+        const int following = min(t + KW, last);
+        scores();
         __builtin_amdgcn_sched_barrier(0);
-        load_keys(b, following, ids[kAhead][0], ids[kAhead][1], more ? k_lane : 0);
-        references(std::false_type());
+        load_keys(following, next0, next1, more ? k_lane : 0);
+        references(std::false_type(), 0);
 #pragma unroll
         for (int k = 0; k < 4; ++k) exponentials(0, k);
 #pragma unroll
-        for (int k = 0; k < 4 * E; ++k) transpose(b, k);
+        for (int k = 0; k < 4 * E; ++k) transpose(k);
         __builtin_amdgcn_sched_barrier(0);
-        load_values(b, following, ids[kAhead][0], ids[kAhead][1], more ? v_lane : 0);
+        load_values(following, next0, next1, more ? v_lane : 0);
         outputs();
         t += KW;
-#pragma unroll
-        for (int i = 0; i <= kAhead; ++i) {
-          ids[i][0] = ids[i + 1][0];
-          ids[i][1] = ids[i + 1][1];
-        }
-        page_ids(min(t + KW * (kAhead + 1), last), ids[kAhead + 1][0], ids[kAhead + 1][1]);
-        return true;
-      };
-      bool odd = false;
-      while (step(0)) {
-        if constexpr (kAhead == 2) {
-          odd = true;
-          if (!step(1)) break;
-          odd = false;
-        }
+        id0 = next0;
+        id1 = next1;
+        next0 = then0;
+        next1 = then1;
+        page_ids(min(t + 2 * KW, last), then0, then1);
       }
-      if (kAhead == 2 && odd && t < t1) {
-#pragma unroll
-        for (int u = 0; u < 2; ++u)
-#pragma unroll
-          for (int c = 0; c < DC; ++c) kf[0][u][c] = kf[kAhead - 1][u][c];
-#pragma unroll
-        for (int j = 0; j < 8; ++j)
-#pragma unroll
-          for (int e = 0; e < EW; ++e) vf[0][j][e] = vf[kAhead - 1][j][e];
-      }
-      id0 = ids[0][0];
-      id1 = ids[0][1];
     }
     // the last cached keys, the new ones, and what lies on and behind pages that are not there
     while (t < t1) {
-      const int key0 = t * kTile;
-      scores(0);
+      const int key0 = t * kTile, me = thread(), row16 = me & 15, of4 = me >> 4 & 3;
+      scores();
       {
         const bool there0 = there(id0) && key0 >> a.log_page < a.max_pages, there1 = there(id1) && (key0 + 16) >> a.log_page < a.max_pages;
         const int left = rq.keys - key0;
@@ -521,26 +664,26 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         // values of keys that no row sees are taken as 0
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
-          const bool on = exist >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1;
+          const bool on = exist >> (16 * (j >> 2) + 4 * of4 + (j & 3)) & 1;
 #pragma unroll
-          for (int e = 0; e < EW; ++e) vf[0][j][e] = on ? vf[0][j][e] : 0;
+          for (int e = 0; e < EW; ++e) vf[j][e] = on ? vf[j][e] : 0;
         }
       }
-      references(std::true_type());
+      references(std::true_type(), of4);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
         for (int k = 0; k < 4; ++k) exponentials(m, k);
       {
         // Infinities and NaN among the values: 0 * inf would reach rows that do not see the key.  Such a key is taken out of
-        // the matrix product and added by the rows that see it; the probabilities pass through this wavefront's part of `so`.
+        // the matrix product and added by the rows that see it.
         uint32_t bad = 0;
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
           bool mine = false;
 #pragma unroll
           for (int e = 0; e < EW; ++e)
-            mine |= (vf[0][j][e] & Matrix<T>::kExponent) == Matrix<T>::kExponent || (vf[0][j][e] >> 16 & Matrix<T>::kExponent) == Matrix<T>::kExponent;
+            mine |= (vf[j][e] & Matrix<T>::kExponent) == Matrix<T>::kExponent || (vf[j][e] >> 16 & Matrix<T>::kExponent) == Matrix<T>::kExponent;
           const uint64_t votes = __ballot(mine);
 #pragma unroll
           for (int k = 0; k < 4; ++k) bad |= (votes >> (16 * k) & 0xFFFF) != 0 ? 1u << (16 * (j >> 2) + 4 * k + (j & 3)) : 0;
@@ -548,8 +691,8 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         if (bad != 0) {
 #pragma unroll 1
           for (uint32_t left = bad; left != 0; left &= left - 1) {
-            const int key = __builtin_ctz(left), j = 4 * (key >> 4) + (key & 3), from = 16 * (key >> 2 & 3) + x16;
-            const T* v = vh + half_offset(key < 16 ? id0 : id1, key0 + (key & 16)) + (key & 15) * D + E * 4 * g;
+            const int key = __builtin_ctz(left), j = 4 * (key >> 4) + (key & 3), from = 16 * (key >> 2 & 3) + row16;
+            const T* v = vh + half_offset(key < 16 ? id0 : id1, key0 + (key & 16)) + (key & 15) * D + E * 4 * of4;
 #pragma unroll
             for (int m = 0; m < MT; ++m) {
               const uint32_t b0 = __shfl(p[m][0], from), b1 = __shfl(p[m][1], from), b2 = __shfl(p[m][2], from), b3 = __shfl(p[m][3], from);
@@ -565,14 +708,14 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
           }
 #pragma unroll
           for (int j = 0; j < 8; ++j) {
-            const bool out = bad >> (16 * (j >> 2) + 4 * g + (j & 3)) & 1;
+            const bool out = bad >> (16 * (j >> 2) + 4 * of4 + (j & 3)) & 1;
 #pragma unroll
-            for (int e = 0; e < EW; ++e) vf[0][j][e] = out ? 0 : vf[0][j][e];
+            for (int e = 0; e < EW; ++e) vf[j][e] = out ? 0 : vf[j][e];
           }
         }
       }
 #pragma unroll
-      for (int k = 0; k < 4 * E; ++k) transpose(0, k);
+      for (int k = 0; k < 4 * E; ++k) transpose(k);
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -582,7 +725,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
     }
 
     // the next segment's first loads are in flight while this one's results meet, where its queries have a place
-    constexpr bool kEarly = !kShared;
+    constexpr bool kEarly = KW == 4 && !kShared;
     const Segment done = now;
     work = next_segment(now);
     if (kEarly && work) open(now);
@@ -599,8 +742,7 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a) {
         store_run<T, E>(static_cast<T*>(a.out) + (int64_t)(done.rq.first_row + tok) * a.out_stride + (done.h * a.group + row - tok * a.group) * D + d, y);
       } else {
         float* to = a.part_o + (slot * kRows + in_chunk) * D + d;
-#pragma unroll
-        for (int n = 0; n < E; n += 2) *reinterpret_cast<float2*>(to + n) = make_float2(y[n], y[n + 1]);
+        __builtin_memcpy(__builtin_assume_aligned(to, E % 4 == 0 ? 16 : 8), y, 4 * E);
       }
     };
     auto put_sums = [&](int in_chunk, float reference, float all) {
@@ -696,7 +838,7 @@ __global__ void __launch_bounds__(256) join_kernel(Attend a) {
   int64_t part = 0, at = 0;
   int64_t* line_ends = reinterpret_cast<int64_t*>(requests + a.requests);
   if constexpr (by_chunk) {
-    part = part_size(a, lay_line(a, line_ends, requests, wave_sums));
+    part = part_size(a, lay_line<4>(a, line_ends, requests, wave_sums));
     at = blockIdx.x;                         // of the chunks of request r and those behind it
   }
   for (;;) {
@@ -776,17 +918,17 @@ __global__ void __launch_bounds__(256) join_kernel(Attend a) {
 template <typename T, int D, int MT, int KW>
 static hipError_t launch_chunks(const Attend& a, const AttendPlan& p, hipStream_t st) {
   const size_t lds = (size_t)a.requests * (sizeof(int64_t) + sizeof(Request));
-  hipLaunchKernelGGL((attend_kernel<T, D, MT, KW>), dim3(p.workgroups), dim3(256), lds, st, a);
+  hipLaunchKernelGGL((attend_kernel<T, D, MT, KW>), dim3(p.workgroups), dim3(KW == 1 ? 512 : 256), lds, st, a);
   return hipGetLastError();
 }
 
 template <typename T, int D>
 hipError_t launch_attend(const Attend& a, const AttendPlan& p, hipStream_t st) {
-  constexpr int kWide = D == 256 ? 2 : 4;
+  constexpr int kWide = D == 256 ? 1 : 2;
   hipError_t e = hipErrorInvalidValue;
   if (a.chunk_rows == 16) e = launch_chunks<T, D, 1, 4>(a, p, st);
   else if (a.chunk_rows == 32) e = launch_chunks<T, D, 2, 4>(a, p, st);
-  else if (a.chunk_rows == 64 * kWide) e = launch_chunks<T, D, kWide, 1>(a, p, st);
+  else if (a.chunk_rows == 128 * kWide) e = launch_chunks<T, D, kWide, 1>(a, p, st);
   else if constexpr (D < 256) e = launch_chunks<T, D, 4, 4>(a, p, st);
   if (e != hipSuccess || a.whole) return e;
   const size_t lds = (size_t)a.requests * (sizeof(int64_t) + sizeof(Request));

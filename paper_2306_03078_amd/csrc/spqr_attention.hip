@@ -11,27 +11,38 @@ SPQR_ATTEND_EXTERN(96)
 SPQR_ATTEND_EXTERN(128)
 SPQR_ATTEND_EXTERN(256)
 
+// Short prefixes: up to here a second launch takes longer than a chunk's tiles one after the other.  64 requests of up to 600 keys, 8
+// key heads of 64 elements: 13.8 us in one launch, 19.9 us cut and joined; equal at about 600 keys where the chunks are few.
 constexpr int kWholeTiles = 20;
+// From these bytes of keys and values on, 256 rows a chunk where a request has more than 64.  Fewer bytes come out of the L2s time and
+// again, and smaller parts fill the card better: 4096 rows over 8000 keys of one head (4 MB) 42 us in chunks of 64, 61 us in chunks
+// of 256, over 32000 keys 108 and 123 us; out of the HBM, up to 512 rows, 4 requests of up to 32000 keys, 8 heads (210 MB),
+// 190 and 138 us.
+constexpr int64_t kFromMemory = 64 << 20;
 
-// Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them.  The hint
-// only chooses; any rows are right with any chunks.
+// Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them (4 rows: 26.8 us
+// in chunks of 16, 28.1 of 32, 30.2 of 64; 16 rows 28.6, 28.8, 31.4 us; 32 rows 30.0 us in 32, 33.0 in 64; 16 requests of up to 4000
+// keys, 8 heads of 128).  The hint only chooses; any rows are right with any chunks.
 static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   AttendPlan p;
   const int64_t rows = (int64_t)(s->max_fresh > 0 ? s->max_fresh : SPQR_MAX_FRESH) * (s->heads / s->kv_heads);
   const int most = s->head_dim == 256 ? 32 : 64;           // rows that one wavefront has registers for
   const int64_t kv_bytes = 4ll * s->requests * s->kv_heads * s->head_dim * min((int64_t)s->max_pages * s->page, (int64_t)s->pages * s->page);
-  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || kv_bytes < (64 << 20) ? most : 4 * most;
+  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || kv_bytes < kFromMemory ? most : 4 * most;
   // What a (key head, chunk) costs beside its tiles, in tiles.  Measured with 4 / 8 / 16 / 24 (16 rows: 52 heads of 16 requests of up
   // to 8192 keys 238 / 222 / 226 / 229 us, 32 heads of 64 elements, 64 requests of up to 1500 76 / 67 / 70 / 74 us); with
   // 8 / 16 / 24 (32 rows: 45.5 / 42.4 / 45.1 us).
   a->start = a->chunk_rows == 16 ? 8 : 16;
-  // as many as run at once: with 16 rows two or (D = 64) three of four wavefronts a CU, else and with D = 256 one
+  // as many as run at once: with 16 rows two or (D = 64; 64 requests of up to 1500 keys, 32 heads: 76 us, two 84 us) three of four
+  // wavefronts a CU, else and with D = 256 one
   p.workgroups = a->chunk_rows > 16 || s->head_dim == 256 ? 256 : s->head_dim == 64 ? 768 : 512;
-  // Short prefixes, by the table's width: a second launch takes longer than a chunk's tiles one after the other.
   a->whole = (int64_t)s->max_pages * s->page <= kWholeTiles * kTile;
   const int64_t live = min(rows, (int64_t)a->chunk_rows);
   const int64_t chunks = (int64_t)s->requests * s->kv_heads * ((rows + a->chunk_rows - 1) / a->chunk_rows);
-  p.by_chunk = chunks * 16 < p.workgroups;
+  // Fewer chunks than cuts: a workgroup a chunk, whose wavefronts share the parts (2 requests of up to 60000 keys of one head: 43 us,
+  // a wavefront a cut 108 us; 4 requests of up to 16000 keys, 8 heads: 28 against 37 us; 16 requests, 52 heads, more chunks
+  // than cuts: equal).
+  p.by_chunk = chunks < p.workgroups;
   p.join_x = p.by_chunk ? (int)chunks : p.workgroups;
   p.join_y = (int)((live + (p.by_chunk ? 3 : 15)) / (p.by_chunk ? 4 : 16));
   return p;
