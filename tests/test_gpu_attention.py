@@ -354,6 +354,55 @@ def test_pages_missing_and_values_masked_under_many_rows(S, D):
     assert bool(torch.isnan(got[:70][sees]).all())
 
 
+@pytest.mark.parametrize("dtype", ["float16", "bfloat16"])
+@pytest.mark.parametrize("D,group,fresh,page", [(64, 71, 3, 16), (96, 16, 5, 32), (128, 8, 40, 64), (256, 8, 9, 128)])
+def test_tiles_shared_by_many_rows(S, dtype, D, group, fresh, page):
+    """Many full tiles in a row, in a workgroup's part and over several: as they are, with a page missing in their middle, and with
+    scores that grow along the prefix."""
+    import torch
+    p = Problem([6000, 777], [fresh, 1], 2 * group, 2, D, page, dtype, "tree", seed=D)
+    step = roomy(p, S)
+    p.check(S.spqr_tree_attention(step, p.q))
+    p.table[0, 2000 // page] = -1
+    step.table.copy_(i32(p.table))
+    p.check(S.spqr_tree_attention(step, p.q))
+    order = torch.arange(6000, dtype=torch.float64) / 6000
+    for j in range(0, 6000, 3):
+        if p.table[0, j // page] >= 0:
+            p.k[0, p.table[0, j // page], 0, j % page] = (p.q[0, 0].double().cpu() * order[j] * 0.4).to(p.dtype).cuda()
+    p.check(S.spqr_tree_attention(step, p.q))
+
+
+def test_values_that_are_not_finite_come_through_shared_tiles(S):
+    """A NaN and an infinity in cached values reach their elements of every row and no other element."""
+    import torch
+    for D in (64, 128, 256):
+        p = Problem([900], [40], 8, 2, D, 16, "bfloat16", "tree")
+        step = roomy(p, S)
+        row = (0, p.table[0, 3], 1, 7)
+        p.v[row][5], p.v[row][D - 2] = math.nan, -math.inf
+        out = S.spqr_tree_attention(step, p.q)
+        assert bool(torch.isnan(out[:, 4:, 5]).all()) and bool((out[:, 4:, D - 2] == -math.inf).all())
+        rest = [d for d in range(D) if d not in (5, D - 2)]
+        assert bool(torch.isfinite(out[:, 4:, rest]).all()) and bool(torch.isfinite(out[:, :4]).all())
+
+
+@pytest.mark.parametrize("D", [64, 256])
+def test_many_requests_of_many_rows(S, D):
+    """As many requests as there can be, their list in LDS beside the tiles."""
+    rng = np.random.default_rng(D)
+    p = Problem(rng.integers(0, 90, 1024), rng.integers(0, 2, 1024), 80, 1, D, 16, "float16", "chain")
+    p.check(S.spqr_tree_attention(roomy(p, S), p.q))
+
+
+def test_many_rows_in_one_launch(S):
+    """Short tables of many requests: nothing is cut, chunks of many rows."""
+    rng = np.random.default_rng(3)
+    p = Problem(rng.integers(0, 600, 110), rng.integers(0, 15, 110), 5, 1, 256, 16, "bfloat16", "tree")
+    p.table = np.concatenate([p.table, np.full((110, 40 - p.table.shape[1]), -1)], axis=1)
+    p.check(S.spqr_tree_attention(p.step(S, max_fresh=14), p.q))
+
+
 def test_same_bits_every_time_on_any_stream_and_from_a_graph(S):
     import torch
     p = Problem([900, 20, 333], [16, 1, 9], 16, 4, 128, 16, "bfloat16", "tree")
