@@ -232,6 +232,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
   constexpr int kStageK = 32 * kST * kKeyRow, kStageV = 4 * kST * D;           // 16-byte places
   __shared__ __align__(16) float shared[KW == 1 ? 8 * (kStageK + kStageV) : kMeet > kQueries ? kMeet : kQueries];
   float(*so)[MT][E][kParts][64][4 / kParts] = reinterpret_cast<float(*)[MT][E][kParts][64][4 / kParts]>(shared);      // [4]
+  __shared__ int taken[2][2];                // by segments in turn, stages in turn
   __shared__ float sm[4][KW == 4 ? kRows : 1], sl[4][KW == 4 ? kRows : 1];
 
   const int tid = threadIdx.x, lane = tid & 63, wave = uniform(tid >> 6), x16 = lane & 15, g = lane >> 4;
@@ -345,6 +346,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
     }
   };
 
+  int segment = 0;
   Segment now;
   bool work = next_segment(now);
   if (work) open(now);
@@ -538,17 +540,22 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
         __builtin_amdgcn_s_barrier();
         __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "workgroup", "local");
       };
-      bool ok0 = stage_ids(at_tile);
-      if (ok0) {
-        fetch(at_tile, true);
-        bool ok1 = stage_ids(at_tile + kST);
-        meet();                                // the last segment's stages are read
+      // Whether a stage is taken: one thread's word for all, so that all meet as often whatever happens to the table meanwhile.
+      bool ok = stage_ids(at_tile);
+      fetch(at_tile, ok);
+      if (tid == 0) taken[segment][0] = ok;
+      ok = stage_ids(at_tile + kST);
+      if (tid == 0) taken[segment][1] = ok;
+      meet();                                  // the last segment's stages are read
+      if (uniform(taken[segment][0])) {
         lay_down(0);
-        fetch(at_tile + kST, ok1);
-        bool ok2 = stage_ids(at_tile + 2 * kST);
+        fetch(at_tile + kST, ok);
+        ok = stage_ids(at_tile + 2 * kST);
+        bool more;
         int b = 0;
         do {
           meet();
+          more = uniform(taken[segment][b ^ 1]);
           const uint32_t me = thread(), x = me & 15, of = me >> 4 & 3;
           const u32x4* keys = stage + b * (kStageK + kStageV) + x * kKeyRow + of;
           const u32x4* values = stage + b * (kStageK + kStageV) + kStageK + of * E * 16;
@@ -592,16 +599,16 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
             if (i + 1 < kST) read_keys(i + 1);
             if (i == 0) {
               lay_down(b ^ 1);
-              fetch(at_tile + 2 * kST, ok2);
-              ok0 = ok1;
-              ok1 = ok2;
-              ok2 = stage_ids(at_tile + 3 * kST);
+              fetch(at_tile + 2 * kST, ok);
+              if (tid == 0) taken[segment][b] = ok;
+              ok = stage_ids(at_tile + 3 * kST);
             }
           }
           at_tile += kST;
           b ^= 1;
-        } while (ok0);
+        } while (more);
       }
+      segment ^= 1;
       if (t < t1) t = at_tile;
       load_tile(min(t, t1 - 1));             // (also where there is none: then no registers keep the last segment's)
     } else if (t < plain_end) {
