@@ -39,10 +39,10 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   a->whole = (int64_t)s->max_pages * s->page <= kWholeTiles * kTile;
   const int64_t live = min(rows, (int64_t)a->chunk_rows);
   const int64_t chunks = (int64_t)s->requests * s->kv_heads * ((rows + a->chunk_rows - 1) / a->chunk_rows);
-  // Fewer chunks than cuts: a workgroup a chunk, whose wavefronts share the parts (2 requests of up to 60000 keys of one head: 43 us,
-  // a wavefront a cut 108 us; 4 requests of up to 16000 keys, 8 heads: 28 against 37 us; 16 requests, 52 heads, more chunks
-  // than cuts: equal).
-  p.by_chunk = chunks < p.workgroups;
+  // Chunks of many parts: workgroups for chunks, whose wavefronts share the parts (2 requests of up to 60000 keys of one head, 256
+  // parts: 43 us, workgroups for cuts 108 us; 4 requests of up to 16000 keys, 8 heads, 16 parts: 29 against 37 us; 8 parts: equal;
+  // 8 requests of up to 8000 keys, 8 heads of 64, chunks of 256 rows in 2 parts: 75 against 49 us).
+  p.by_chunk = chunks * 16 <= p.workgroups;
   p.join_x = p.by_chunk ? (int)chunks : p.workgroups;
   p.join_y = (int)((live + (p.by_chunk ? 3 : 15)) / (p.by_chunk ? 4 : 16));
   return p;
