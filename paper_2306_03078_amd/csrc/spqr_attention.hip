@@ -17,7 +17,7 @@ constexpr int kWholeTiles = 20;
 // From these bytes of keys and values on, 256 rows a chunk where a request has more than 64.  Fewer bytes come out of the L2s time and
 // again, and smaller parts fill the card better: 4096 rows over 8000 keys of one head (4 MB) 42 us in chunks of 64, 61 us in chunks
 // of 256, over 32000 keys 108 and 123 us; out of the HBM, up to 512 rows, 4 requests of up to 32000 keys, 8 heads (210 MB),
-// 190 and 129 us.
+// 190 and 132 us.
 constexpr int64_t kFromMemory = 64 << 20;
 
 // Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them (4 rows: 26.8 us

@@ -71,8 +71,9 @@ class SpQRStep:
     k_cache, v_cache: [layers, pages, kv_heads, page, head_dim] float16 or bfloat16 device tensors (None for a step that
     is only planned: give page and pages).  heads: query heads.  requests, tokens, max_pages: sizes, where no array given says
     them.  Any array of include/spqr_serve.h can be given by its name; the others are made here: empty requests, and an
-    empty table with a ring that has all pages (pool and ends are only made with a table).  parent (int32 [tokens]) is None unless given, mask exists where mask_words > 0
-    or it is given.  rotary: float32 [positions, rotary_dim], cosines, then sines, or None.  scale: head_dim ** -0.5 if None.
+    empty table with a ring that has all pages (pool and ends are only made with a table).  parent (int32 [tokens]) is None
+    unless given, mask exists where mask_words > 0 or it is given.  rotary: float32 [positions, rotary_dim], cosines, then
+    sines, or None.  scale: head_dim ** -0.5 if None.
     The step keeps the tensors alive and owns the attention's scratch: use it on one stream at a time."""
 
     def __init__(self, k_cache, v_cache, heads=1, *, requests=None, tokens=None, max_pages=None, page=None, pages=None, mask_words=None,
