@@ -106,7 +106,9 @@ int spqr_cache_plan(const spqr_step_t* s, void* stream);
 /* For every row t with 0 <= position[t] (< rotary_positions where there is a rotation): q_out[t] = q[t] turned by its
  * position, in the cache's type; k[t] turned and v[t] go to slot[t] of `layer` (nowhere if the slot is not in the
  * cache).  Turning (a, b) by position p: (a c - b s, b c + a s), c = rotary[p][i], s = rotary[p][rotary_dim / 2 + i],
- * in binary32, rounded once to the cache's type.  Other rows: q_out[t] = 0, nothing stored.
+ * in binary32, rounded once to the cache's type.  Other rows: q_out[t] = 0, nothing stored.  (Rows whose mask has such a
+ * token see what its place held before, if its page is there: what the attention gives for rows with a position behind
+ * the end of `rotary` means nothing.)
  * `x` is read during the call (a HOST structure); its rows are aligned to their type (where all addresses are multiples of
  * 16 bytes they are read faster).  q_out [tokens][heads][head_dim], 16-byte aligned, overlaps none of them.  Two rows
  * with one slot: undefined which stays. */
@@ -130,8 +132,10 @@ int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const void* q, int6
 /* last[r] is the last accepted new token of request r (in-request index; none if it is no row of r): the tokens of its
  * mask are the accepted path (0 .. last[r] without masks; every new token with last = NULL).  The a-th token of the path
  * moves from key cached + its index to key cached + a, k and v, in all layers; cached_out[r] = cached[r] + the
- * path's length.  Reads cached, table, q_start, mask; pages stay as spqr_cache_plan laid them (the next plan gives back
- * what is no longer needed). */
+ * path's length.  The path ends before its first token that spqr_cache_store left out (its slot not in the cache; its
+ * position below 0 or, where there is a rotation, no row of `rotary`) or for which the cache has no place: lengths cover
+ * stored tokens only, also where pages were lacking.  Reads cached, table, q_start, mask, slot, position (NULL for one of
+ * these two: not looked at); pages stay as spqr_cache_plan laid them (the next plan gives back what is no longer needed). */
 int spqr_cache_keep(const spqr_step_t* s, const int32_t* last, void* stream);
 
 #ifdef __cplusplus

@@ -147,6 +147,10 @@ __global__ void __launch_bounds__(256) plan_kernel(spqr_step_t s) {
 // ---------------------------------------------------------------------------------------------------------------------
 // Rotary embedding, store.
 // ---------------------------------------------------------------------------------------------------------------------
+// What spqr_cache_store does with a row, and spqr_cache_keep counts by: a row is in use; its k and v have a place in the cache.
+__device__ __forceinline__ bool row_in_use(int position, int rot, int positions) { return position >= 0 && (rot == 0 || position < positions); }
+__device__ __forceinline__ bool in_cache(int slot, int slots) { return slot >= 0 && slot < slots; }
+
 struct Store {
   spqr_rows_t x;
   void *q_out, *kc, *vc;         // the caches: those of the layer
@@ -178,9 +182,9 @@ __global__ void __launch_bounds__(256) store_kernel(Store a) {
   if (head0 >= lanes) return;
   const int64_t t = blockIdx.x;
   const int pos = a.position[t];
-  const bool live = pos >= 0 && (a.rot == 0 || pos < a.positions);
+  const bool live = row_in_use(pos, a.rot, a.positions);
   const int slot = a.slot[t];
-  const bool stored = live && slot >= 0 && slot < a.slots;
+  const bool stored = live && in_cache(slot, a.slots);
   const int half = a.rot / 2;
   const bool turns = live && o < a.rot, upper = o >= half;
   const int partner = a.pairs ? (V == 1 ? o ^ 1 : o) : upper ? o - half : o + half;
@@ -259,7 +263,8 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
 __global__ void __launch_bounds__(256) keep_kernel(spqr_step_t s, const int32_t* __restrict__ last, int64_t columns) {
   __shared__ int64_t from[SPQR_MAX_FRESH], to[SPQR_MAX_FRESH];
-  __shared__ int moved_from;
+  __shared__ bool has_slot[SPQR_MAX_FRESH];
+  __shared__ int moved_from, path_end;
   const int r = blockIdx.x, tid = threadIdx.x, log_page = __ffs(s.page) - 1;
   const int base = clamp_to(s.q_start[r], s.tokens), end = clamp_to(s.q_start[r + 1], s.tokens);
   const int rows = min(max(0, end - base), SPQR_MAX_FRESH);
@@ -267,23 +272,30 @@ __global__ void __launch_bounds__(256) keep_kernel(spqr_step_t s, const int32_t*
   const int leaf = last == nullptr ? rows - 1 : last[r];
   const bool path = leaf >= 0 && leaf < rows;
   const bool by_mask = last != nullptr && s.mask_words > 0;
-  int count = path ? leaf + 1 : 0;
+  const bool slotted = tid < rows && (s.slot == nullptr || in_cache(s.slot[base + tid], s.pages * s.page));
+  const bool stored = slotted && (s.position == nullptr || row_in_use(s.position[base + tid], s.rotary_dim, s.rotary_positions));
+  // thread j: token j is on the path as the rank-th
+  int count = path ? leaf + 1 : 0, rank = tid;
+  bool on = tid < count;
   if (by_mask) {
-    // thread j: token j is on the path as the rank-th
-    int rank = 0, all = 0;
-    bool on = false;
+    rank = count = 0;
+    on = false;
     for (int w = 0; path && w < s.mask_words; ++w) {
       uint64_t m = s.mask[(int64_t)(base + leaf) * s.mask_words + w];
       const int n = min(max(rows - 64 * w, 0), 64);
       m = n == 0 ? 0 : m & (~0ull >> (64 - n));
-      all += __popcll(m);
+      count += __popcll(m);
       if (w < tid >> 6) rank += __popcll(m);
       if (w == tid >> 6) { rank += __popcll(m & ((1ull << (tid & 63)) - 1)); on = m >> (tid & 63) & 1; }
     }
-    count = all;
-    if (tid == 0) moved_from = count;
-    __syncthreads();
-    if (on) {
+  }
+  has_slot[tid] = slotted;
+  if (tid == 0) moved_from = path_end = count;
+  __syncthreads();
+  if (on) {
+    // The path ends at its first token that was not stored, or for which there is no place.
+    if (!stored || !has_slot[rank]) atomicMin(&path_end, rank);
+    if (by_mask) {
       // (page id, row) of a key as a row of a page-and-head grid; -1 where there is none
       auto place = [&](int64_t key) -> int64_t {
         const int64_t at = key >> log_page;
@@ -295,8 +307,9 @@ __global__ void __launch_bounds__(256) keep_kernel(spqr_step_t s, const int32_t*
       if (from[rank] < 0 || to[rank] < 0) from[rank] = to[rank] = -1;
       if (tid > rank) atomicMin(&moved_from, rank);      // the first that moves; all behind it do
     }
-    __syncthreads();
   }
+  __syncthreads();
+  count = path_end;
   if (blockIdx.y == 0 && tid == 0) s.cached_out[r] = (int32_t)min(cached + count, (int64_t)0x7FFFFFFF);
   if (!by_mask) return;
   const int64_t column = (int64_t)blockIdx.y * 256 + tid;
@@ -374,7 +387,7 @@ extern "C" int spqr_cache_keep(const spqr_step_t* s, const int32_t* last, void* 
   if (rc) return rc;
   if (!s->cached || !s->table || !s->q_start || !s->cached_out || (s->mask_words > 0 && !s->mask)) return SPQR_ERR_NULL;
   if (!aligned(s->cached, 4) || !aligned(s->table, 4) || !aligned(s->q_start, 4) || !aligned(s->cached_out, 4) || !aligned(s->mask, 8) ||
-      !aligned(last, 4))
+      !aligned(s->slot, 4) || !aligned(s->position, 4) || !aligned(last, 4))
     return SPQR_ERR_ALIGN;
   if (s->cached == s->cached_out) return SPQR_ERR_PARAM;                         // read by all workgroups, written by one
   const bool moves = last != nullptr && s->mask_words > 0;

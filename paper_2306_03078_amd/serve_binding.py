@@ -248,7 +248,8 @@ def spqr_tree_attention(step: SpQRStep, q, layer: int = 0, out=None, stream=None
 
 def spqr_cache_keep(step: SpQRStep, last=None, stream=None):
     """After verification: last [requests] int32, the last accepted new token of each request (-1: none), or None: all.  The
-    accepted rows move together in all layers; returns step.cached_out, the new lengths."""
+    accepted rows move together in all layers; returns step.cached_out, the new lengths (up to the first token that was not stored:
+    where pages were lacking, the lengths grow by less than the path)."""
     import torch
     if last is not None and (last.dtype != torch.int32 or not last.is_contiguous() or last.numel() != step.requests or not last.is_cuda):
         raise ValueError(f"last: a contiguous int32 device tensor [{step.requests}]")
