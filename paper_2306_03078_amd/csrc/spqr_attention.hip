@@ -80,7 +80,8 @@ extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const vo
   if (rc) return rc;
   if (layer < 0 || layer >= s->layers) return SPQR_ERR_PARAM;
   if (!q || !out || !s->cached || !s->table || !s->q_start || (s->mask_words > 0 && !s->mask) || !s->workspace) return SPQR_ERR_NULL;
-  if (!std::isfinite(s->scale)) return SPQR_ERR_PARAM;
+  const float scale2 = std::fabs(s->scale) * 1.4426950408889634f;
+  if (!std::isfinite(scale2)) return SPQR_ERR_PARAM;
   const int64_t row = (int64_t)s->heads * s->head_dim;
   if (q_stride < row || out_stride < row) return SPQR_ERR_SHAPE;
   if (!aligned(q, 16) || !aligned(out, 16) || q_stride % 8 != 0 || out_stride % 8 != 0 || !aligned(s->cached, 4) || !aligned(s->table, 4) ||
@@ -99,8 +100,9 @@ extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const vo
   a.part_ml = a.part_o + 2ll * p.workgroups * a.chunk_rows * s->head_dim;
   a.requests = s->requests; a.tokens = s->tokens; a.kv_heads = s->kv_heads; a.group = s->heads / s->kv_heads;
   a.log_page = __builtin_ctz(s->page); a.pages = s->pages; a.max_pages = s->max_pages; a.words = s->mask_words;
-  a.scale2 = std::fabs(s->scale) * 1.4426950408889634f;
+  a.scale2 = scale2 > 0.f ? scale2 : 1.f;
   a.turn = s->scale < 0.f ? 0x80008000u : 0u;
+  a.counts = scale2 > 0.f ? ~0u : 0u;
   a.inv_group = 1.0f / (float)a.group;
   a.workgroups = p.workgroups;
   a.inv_workgroups = 1.0 / p.workgroups;
