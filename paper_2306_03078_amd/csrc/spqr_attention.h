@@ -8,9 +8,12 @@
 // exchanges 16-bit halves between its own registers; the n-th instruction then takes the n-th element of each lane.
 // A key's bytes are read once for all rows of a chunk (16 to 256: tokens times the query heads of one key head).
 //
-// The softmax's reference m of a row moves only when a score passes it by 8 (in powers of two; probabilities stay below
-// 2^8): a tile then costs no exchange between lanes.  Sums of probabilities are binary32 and of the unrounded ones, a
-// partial sum a lane; probabilities are rounded to the cache's type for the matrix cores, as their other operand is of it.
+// The softmax's reference m of a row is put kLift below the largest score (in powers of two) and moves only when a score passes it
+// by kLift + 8: a tile then costs no exchange between lanes.  Probabilities stay below 2^(kLift + 8); binary16 has 2^15 as its largest
+// power, so 7 there: keys of 2^-32 of the largest probability still count (2^-25 without: 600 light keys beside a heavy one lost
+// a quarter of their share), and all above 2^-21 with 11 bits.  bfloat16 has binary32's range and needs none.  Sums of probabilities
+// are binary32 and of the unrounded ones, a partial sum a lane; probabilities are rounded to the cache's type for the matrix
+// cores, as their other operand is of it.
 //
 // Work is a line of tiles (request, key head, chunk of rows, 32 keys) that is cut into equal parts, one a workgroup, wherever
 // the cuts fall: lengths are known on the card only.  What a cut divides goes to the workspace as a partial result
@@ -84,6 +87,7 @@ template <> struct Matrix<_Float16> {
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
   }
   static constexpr uint32_t kExponent = 0x7C00;
+  static constexpr float kLift = 7.f;
 };
 template <> struct Matrix<__bf16> {
   typedef __bf16 x8 __attribute__((ext_vector_type(8)));
@@ -92,6 +96,7 @@ template <> struct Matrix<__bf16> {
     return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(x8, a), __builtin_bit_cast(x8, b), c, 0, 0, 0);
   }
   static constexpr uint32_t kExponent = 0x7F80;
+  static constexpr float kLift = 0.f;
 };
 
 template <typename T>
@@ -391,6 +396,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
     };
     auto references = [&](auto masked_tile, int of4) {  // where scores are too large for a row's reference, a new one
       constexpr bool masked = decltype(masked_tile)::value;
+      constexpr float lift = Matrix<T>::kLift;
       float most[MT];
       bool moves = false;
 #pragma unroll
@@ -402,14 +408,14 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
         }
         const f32x4 x = s[m][0], y = s[m][1];
         most[m] = max3(max3(x[0], x[1], x[2]), max3(x[3], y[0], y[1]), max3(y[2], y[3], y[3])) * a.scale2;
-        moves |= most[m] > top[m] + 8.f;
+        moves |= most[m] > top[m] + (lift + 8.f);
       }
       if (__any(moves)) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           most[m] = fmaxf(most[m], __shfl_xor(most[m], 16));
           most[m] = fmaxf(most[m], __shfl_xor(most[m], 32));
-          const float now = most[m] > top[m] + 8.f ? most[m] : top[m];
+          const float now = most[m] > top[m] + (lift + 8.f) ? most[m] - lift : top[m];
           const float back = now == top[m] ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
           top[m] = now;
           sum[m] *= back;
