@@ -9,7 +9,7 @@ import ctypes as C
 import math
 
 from . import binding as B
-from .binding import SPQR_F16, SPQR_F32, SpQRError, _stream_ptr, load_library
+from .binding import SPQR_F16, SPQR_F32, SpQRError, load_library
 
 SPQR_BF16 = 2
 SPQR_MAX_REQUESTS, SPQR_MAX_FRESH = 1024, 256
@@ -31,9 +31,11 @@ class spqr_rows_t(C.Structure):
 
 _entry = {}
 _dtypes = {}
+_current_device = _raw_stream = _int32 = None       # torch's, where this torch has the raw calls (see binding._stream_ptr)
 
 
 def _lib():
+    global _current_device, _raw_stream, _int32
     lib = load_library()
     if not _entry:
         import torch
@@ -45,13 +47,22 @@ def _lib():
             _entry[name] = f if B._call is B._ctypes_call else C.cast(f, C.c_void_p).value
         lib.spqr_tree_attention_workspace_bytes.restype = i64
         lib.spqr_tree_attention_workspace_bytes.argtypes = [S]
+        _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", lambda index: torch.cuda.current_stream(index).cuda_stream)
+        _int32 = torch.int32
         _dtypes.update({torch.float32: SPQR_F32, torch.float16: SPQR_F16, torch.bfloat16: SPQR_BF16})
     return lib
 
 
-def _check(rc, where):
+def _run(name, step, stream, *args):
+    """One of the entries, on the step's device: launches go to the current one, on its current stream where none is given."""
+    if _current_device() != step._index:
+        import torch
+        with torch.cuda.device(step._index):
+            return _run(name, step, stream, *args)
+    rc = B._call(_entry[name], step.desc, *args, _raw_stream(step._index) if stream is None else stream.cuda_stream)
     if rc != 0:
-        raise SpQRError(int(rc), where)
+        raise SpQRError(int(rc), name)
 
 
 # the arrays of a descriptor: their type, and their shape in terms of the step's sizes
@@ -121,8 +132,11 @@ class SpQRStep:
         if not math.isfinite(d.scale):
             raise ValueError(f"scale: a finite number, not {scale}")
         self.device = torch.device(device)
+        if self.device.type != "cuda":
+            raise ValueError(f"a step's arrays are in device memory, not on {self.device}")
         if self.device.index is None:
-            self.device = torch.device(self.device.type, torch.cuda.current_device())
+            self.device = torch.device("cuda", torch.cuda.current_device())
+        self._index = self.device.index
 
         def on_device(a):
             return a.device == self.device
@@ -164,7 +178,7 @@ class SpQRStep:
             self.workspace = torch.empty(max(need, 256), dtype=torch.uint8, device=self.device)
             d.workspace, d.workspace_bytes = self.workspace.data_ptr(), self.workspace.numel()
         T, D = self.tokens, self.head_dim
-        self._q_like, self._kv_like = (((T, h, D), (h * D, D, 1)) for h in (self.heads, self.kv_heads))
+        self._q_like, self._kv_like = (((T, h, D), (h * D, D, 1), self._index) for h in (self.heads, self.kv_heads))
         self._q_of = torch.empty(1, dtype=self.dtype, device=self.device).expand(T, self.heads, D)
         self._rows = spqr_rows_t()
         self._rows_at = C.addressof(self._rows)
@@ -182,15 +196,15 @@ class SpQRStep:
 
 def spqr_cache_plan(step: SpQRStep, stream=None) -> SpQRStep:
     """Pages, slots, positions and masks of a step's new tokens: fills table, q_start, slot, position, mask, held_out, ends_out."""
-    rc = B._call(_entry["spqr_cache_plan"], step.desc, _stream_ptr(stream))
-    if rc != 0:
-        _check(rc, "spqr_cache_plan")
+    _run("spqr_cache_plan", step, stream)
     return step
 
 
 def _row_stride(x, like, name):
     """Elements between the rows of x: [tokens, heads, head_dim] or [tokens, heads * head_dim], each row contiguous.  like: the
-    shape and strides of the dense one."""
+    shape and strides of the dense one, and the device's index."""
+    if x.get_device() != like[2]:
+        raise ValueError(f"{name}: a tensor on cuda:{like[2]}, not on {x.device}")
     shape, strides = x.shape, x.stride()
     if shape == like[0] and strides == like[1]:
         return strides[0]
@@ -207,7 +221,6 @@ def _row_stride(x, like, name):
 def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=None):
     """q turned by its rows' positions (a tensor of the cache's type [tokens, heads, head_dim], returned); k turned, and v,
     stored in their slots of `layer`.  q, k, v: float32, float16 or bfloat16, rows of one step's products."""
-    import torch
     x = step._rows
     dtype = q.dtype
     if dtype not in _dtypes or k.dtype != dtype or v.dtype != dtype:
@@ -217,12 +230,11 @@ def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=N
     x.v_stride = _row_stride(v, step._kv_like, "v")
     x.q, x.k, x.v, x.x_dtype = q.data_ptr(), k.data_ptr(), v.data_ptr(), _dtypes[dtype]
     if out is None:
+        import torch
         out = torch.empty_like(step._q_of, memory_format=torch.contiguous_format)
-    elif out.dtype != step.dtype or not out.is_contiguous() or out.numel() != step._q_of.numel():
-        raise ValueError(f"out: a contiguous {step.dtype} tensor {list(step._q_like[0])}")
-    rc = B._call(_entry["spqr_cache_store"], step.desc, layer, step._rows_at, out, _stream_ptr(stream))
-    if rc != 0:
-        _check(rc, "spqr_cache_store")
+    elif out.dtype != step.dtype or not out.is_contiguous() or out.numel() != step._q_of.numel() or out.get_device() != step._index:
+        raise ValueError(f"out: a contiguous {step.dtype} tensor {list(step._q_like[0])} on {step.device}")
+    _run("spqr_cache_store", step, stream, layer, step._rows_at, out)
     return out
 
 
@@ -240,9 +252,7 @@ def spqr_tree_attention(step: SpQRStep, q, layer: int = 0, out=None, stream=None
         if out.dtype != step.dtype:
             raise ValueError(f"out: {step.dtype}, not {out.dtype}")
         out_stride = _row_stride(out, step._q_like, "out")
-    rc = B._call(_entry["spqr_tree_attention"], step.desc, layer, q, q_stride, out, out_stride, _stream_ptr(stream))
-    if rc != 0:
-        _check(rc, "spqr_tree_attention")
+    _run("spqr_tree_attention", step, stream, layer, q, q_stride, out, out_stride)
     return out
 
 
@@ -250,10 +260,8 @@ def spqr_cache_keep(step: SpQRStep, last=None, stream=None):
     """After verification: last [requests] int32, the last accepted new token of each request (-1: none), or None: all.  The
     accepted rows move together in all layers; returns step.cached_out, the new lengths (up to the first token that was not stored:
     where pages were lacking, the lengths grow by less than the path)."""
-    import torch
-    if last is not None and (last.dtype != torch.int32 or not last.is_contiguous() or last.numel() != step.requests or not last.is_cuda):
-        raise ValueError(f"last: a contiguous int32 device tensor [{step.requests}]")
-    rc = B._call(_entry["spqr_cache_keep"], step.desc, last, _stream_ptr(stream))
-    if rc != 0:
-        _check(rc, "spqr_cache_keep")
+    if last is not None and (last.dtype != _int32 or not last.is_contiguous() or last.numel() != step.requests
+                             or last.get_device() != step._index):
+        raise ValueError(f"last: a contiguous int32 tensor [{step.requests}] on {step.device}")
+    _run("spqr_cache_keep", step, stream, last)
     return step.cached_out
