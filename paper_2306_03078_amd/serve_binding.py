@@ -215,7 +215,7 @@ def _row_stride(x, like, name):
         fits = shape == (tokens, row) and strides[1] == 1
     if not fits:
         raise ValueError(f"{name}: [{tokens}, {heads}, {head_dim}] with contiguous rows, not {list(shape)} with strides {list(strides)}")
-    return strides[0] if tokens > 1 else max(strides[0], row)
+    return strides[0] if tokens > 1 else row
 
 
 def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=None):
