@@ -57,8 +57,7 @@ typedef struct spqr_step_t {
   int32_t rotary_dim;            /* leading elements of a head that are rotated, even, <= head_dim; 0: none           */
   int32_t rotary_positions;      /* rows of `rotary`                                                                  */
   int32_t rotary_pairs;          /* 0: element i turns with i + rotary_dim / 2; 1: element 2i with 2i + 1              */
-  float scale;                   /* of the scores, finite, and times log2(e) too; 0: a row's query does not count, all keys
-                                    that it sees count the same                                                        */
+  float scale;                   /* of the scores, finite, and times log2(e) too; 0: all keys that a row sees count the same  */
   void* k;
   void* v;
   const int32_t* cached;         /* [requests]                                                                        */

@@ -48,8 +48,6 @@ struct Attend {
   int requests, tokens, group, kv_heads, log_page, pages, max_pages, words;
   float scale2;                  // |scale| * log2(e), > 0
   uint32_t turn;                 // 0x80008000 where scale < 0: queries change their signs
-  uint32_t counts;               // ~0; 0 where scale = 0: queries are taken as 0, at scale2 = 1 (what a row does not see is -inf before
-                                 // the scale, and 0 * inf is none of the numbers that keep it out)
   float inv_group;
   int workgroups;
   int chunk_rows, start;         // of a chunk; places of the line in front of its tiles
@@ -332,7 +330,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
     auto query = [&](int m, int c) {         // (rows that are none: the last one, without a branch, taken as 0)
       const int row = x.row0 + min(16 * m + x16, x.live_rows - 1), tok = token_of(a, row);
       const T* from = static_cast<const T*>(a.q) + (int64_t)(x.rq.first_row + tok) * a.q_stride + (x.h * a.group + row - tok * a.group) * D + 8 * g;
-      const uint32_t live = 16 * m + x16 < x.live_rows ? a.counts : 0u;
+      const uint32_t live = 16 * m + x16 < x.live_rows ? ~0u : 0u;
       return (*reinterpret_cast<const u32x4*>(from + 32 * c) ^ a.turn) & live;
     };
 #pragma unroll
