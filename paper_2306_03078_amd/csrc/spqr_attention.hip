@@ -21,6 +21,12 @@ constexpr int kWholeTiles = 20;
 // again, and smaller parts fill the card better: 4096 rows over 8000 keys of one head (4 MB) 42 us in chunks of 64, 61 us in chunks
 // of 256, over 32000 keys 108 and 123 us; out of the HBM, up to 512 rows, 4 requests of up to 32000 keys, 8 heads (210 MB),
 // 190 and 132 us.
+// Counted twice: what the requests may read one after another, and what the cache has, which may be less (tables as wide as a pool
+// that many share).  With chunks of 64 in plenty the latter says less, as a workgroup takes several of them one after the other: half
+// of it is enough at 256 of them, any of it above, where a small pool loses less than many small chunks.  In chunks of 64 and 256,
+// tables as wide as the pool: 64 requests of 128 rows over 2 MB 25 and 32 us; 2 of 512 rows, 8 heads, 60 MB 62 and 75 us; 4 of them,
+// 28 MB 45 and 49 us, 60 MB 80 and 69 us; 8 of them, 16 MB 38 and 44 us, 60 MB 95 and 72 us; 32 of 80 rows, 14 MB 24 and 19 us,
+// 60 MB 36 and 28 us.
 constexpr int64_t kFromMemory = 64 << 20;
 
 // Rows of a chunk: as few as hold the rows of a request's key head, so that keys and values are read once for them (4 rows: 26.8 us
@@ -30,8 +36,11 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   AttendPlan p;
   const int64_t rows = (int64_t)(s->max_fresh > 0 ? s->max_fresh : SPQR_MAX_FRESH) * (s->heads / s->kv_heads);
   const int most = s->head_dim == 256 ? 32 : 64;           // rows that one wavefront has registers for
-  const int64_t kv_bytes = 4ll * s->requests * s->kv_heads * s->head_dim * min((int64_t)s->max_pages * s->page, (int64_t)s->pages * s->page);
-  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || kv_bytes < kFromMemory ? most : 4 * most;
+  const int64_t page_bytes = 4ll * s->kv_heads * s->head_dim * s->page, read = s->requests * page_bytes * min(s->max_pages, s->pages);
+  const int64_t there = page_bytes * min((int64_t)s->requests * s->max_pages, (int64_t)s->pages);
+  const int64_t small = (int64_t)s->requests * s->kv_heads * ((rows + most - 1) / most);        // chunks of `most` rows
+  const bool from_memory = read >= kFromMemory && (small > 256 || there >= kFromMemory * 128 / max(small, (int64_t)128));
+  a->chunk_rows = rows <= 16 ? 16 : rows <= 32 ? 32 : rows <= most || !from_memory ? most : 4 * most;
   // What a (key head, chunk) costs beside its tiles, in tiles.  Measured with 4 / 8 / 16 / 24 (16 rows: 52 heads of 16 requests of up
   // to 8192 keys 238 / 222 / 226 / 229 us, 32 heads of 64 elements, 64 requests of up to 1500 76 / 67 / 70 / 74 us); with
   // 8 / 16 / 24 (32 rows: 45.5 / 42.4 / 45.1 us).
