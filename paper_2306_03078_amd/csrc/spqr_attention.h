@@ -19,11 +19,11 @@
 // the cuts fall: lengths are known on the card only.  What a cut divides goes to the workspace as a partial result
 // and join_kernel adds the parts in their order.
 //
-// What bounds it.  Few rows: memory; 16 requests of up to 8192 keys, 52 heads of 128 elements, reads 1.25 GB in 220 us, 5.7 TB/s
+// What bounds it.  Few rows: memory; 16 requests of up to 8192 keys, 52 heads of 128 elements, reads 1.25 GB in 223 us, 5.6 TB/s
 // (a copy reads and writes 4.7 TB/s); 40 rows over 131067 keys, 8 heads, 537 MB in 108 us, 5.0 TB/s.  Short prefixes: two launches
 // and four trips to memory one after the other (lengths, pages, keys, parts); 1024 keys, 32 heads 15.7 us.  Many rows: issue of
 // the matrix cores' and the softmax's instructions; 4096 rows over 260000 keys 580 us, 940 TFLOP/s; 4 requests of up to 64
-// tokens, 64 heads on 8, up to 32000 keys 132 us, 540 TFLOP/s (chunks in part empty, parts written and joined).
+// tokens, 64 heads on 8, up to 32000 keys 130 us, 550 TFLOP/s (chunks in part empty, parts written and joined).
 #ifndef SPQR_ATTENTION_INTERNAL_H_
 #define SPQR_ATTENTION_INTERNAL_H_
 #include <cmath>
@@ -464,7 +464,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
       // is full.
       // Measured against four wavefronts of 64 rows that each load every tile (KW = 4's way): 512 rows, 8 heads of 128 over up to
       // 32000 keys, 4 requests 142 -> 132 us; 4096 rows over 260000 keys of one head 631 -> 580 us (940 TFLOP/s); heads of 64
-      // elements 60 -> 49 us, of 256 194 -> 154 us.  Dropped, by the first of these: two stages on their way with the
+      // elements 60 -> 49 us, of 256 194 -> 154 us (where 160 to 190 bytes of a lane's registers do not fit and go to memory).  Dropped, by the first of these: two stages on their way with the
       // queries in LDS, in whose registers they are (12 % slower), priorities around the products (1 %), halves of the wavefronts
       // half a stage apart (8 %), half-full chunks' tiles shared among twice the wavefronts (equal).
       constexpr int kK = (4 * kST * D + 511) / 512, kV = (2 * kST * D + 511) / 512;

@@ -45,8 +45,9 @@ static AttendPlan plan_attend(const spqr_step_t* s, Attend* a) {
   // to 8192 keys 238 / 222 / 226 / 229 us, 32 heads of 64 elements, 64 requests of up to 1500 76 / 67 / 70 / 74 us); with
   // 8 / 16 / 24 (32 rows: 45.5 / 42.4 / 45.1 us).
   a->start = a->chunk_rows == 16 ? 8 : 16;
-  // as many as run at once: with 16 rows two or (D = 64; 64 requests of up to 1500 keys, 32 heads: 76 us, two 84 us) three of four
-  // wavefronts a CU, else and with D = 256 one
+  // With 16 rows as many as run at once: two or (D = 64; 64 requests of up to 1500 keys, 32 heads: 76 us, two 84 us) three of four
+  // wavefronts a CU.  Else and with D = 256 one a CU: registers leave room for no more, but for chunks of 32 rows with D = 64, two of which
+  // would fit (not measured).
   p.workgroups = a->chunk_rows > 16 || s->head_dim == 256 ? 256 : s->head_dim == 64 ? 768 : 512;
   a->whole = (int64_t)s->max_pages * s->page <= kWholeTiles * kTile;
   const int64_t live = min(rows, (int64_t)a->chunk_rows);

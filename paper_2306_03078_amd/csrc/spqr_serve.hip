@@ -257,7 +257,8 @@ static int store_from(int x_dtype, const Store& a, int tokens, bool wide, hipStr
 // A workgroup finds the path of its request and moves 256 columns of 16 bytes, each thread its column row by row: the path ascends
 // and its a-th entry is at least a, so a row is read before it is overwritten as long as rows are taken in order, eight
 // loads ahead of their stores included.  A trip to memory a group of eight rows and one for the path bound it: 4 rows of 32 layers of
-// 32 heads of 128 elements 4.6 us; 32 requests of 7 rows, 48 layers of 8 heads (44 MB read and written) 12 us, 3.6 TB/s.
+// 32 heads of 128 elements 4.5 us; 32 requests of 7 rows, 48 layers of 8 heads (44 MB read and written) 13 us, 3.3 TB/s.
+// What spqr_cache_store left out is asked for beside the path, in the same trip (0.3 us of the second).
 constexpr int kAhead = 8;
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 
