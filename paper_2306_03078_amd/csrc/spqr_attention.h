@@ -46,7 +46,7 @@ struct Attend {
   Join* joins;                   // [workgroups]
   float *part_o, *part_ml;       // [2 * workgroups][rows of a chunk][D], [...][2]: reference, sum
   int requests, tokens, group, kv_heads, log_page, pages, max_pages, words;
-  float scale2;                  // |scale| * log2(e), > 0
+  float scale2;                  // |scale| * log2(e)
   uint32_t turn;                 // 0x80008000 where scale < 0: queries change their signs
   float inv_group;
   int workgroups;
@@ -67,6 +67,7 @@ template <typename T, int D> hipError_t launch_attend(const Attend& a, const Att
 
 constexpr int kTile = 32;        // keys
 constexpr int kLeast = 4;        // of the line, a part: a tile a wavefront
+constexpr float kFar = 1 << 20;  // a reference beyond it, either way: see `far`
 
 #ifdef __HIP_DEVICE_COMPILE__
 #define SPQR_SCALAR __attribute__((address_space(4)))
@@ -360,13 +361,20 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
     const int live_rows = now.live_rows, t1 = now.t1;
     f32x4 o[MT][E];
     float top[MT], sum[MT];
+    auto nothing = [&] {
 #pragma unroll
-    for (int m = 0; m < MT; ++m) {
-      top[m] = -INFINITY;
-      sum[m] = 0.f;
+      for (int m = 0; m < MT; ++m) {
+        top[m] = -INFINITY;
+        sum[m] = 0.f;
 #pragma unroll
-      for (int n = 0; n < E; ++n) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
-    }
+        for (int n = 0; n < E; ++n) o[m][n] = f32x4{0.f, 0.f, 0.f, 0.f};
+      }
+    };
+    nothing();
+    // Some row's reference in the loops without masks is so large that its own rounding is what an exponent would be made of (a fused
+    // score * scale - reference is off by up to half of its last place): the wavefront takes all its tiles through the loop with
+    // masks once more, which rounds the product as the reference was, so that differences are exact.
+    bool far = false;
 
     // The steps of a tile.  All 16 * MT rows are computed, also those that are none: straight code, in which the matrix cores'
     // work and the rest alternate as written (a wavefront issues in order, and on chunks of 64 rows it is alone on its
@@ -393,27 +401,29 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
       }
     };
     auto references = [&](auto masked_tile, int of4) {  // where scores are too large for a row's reference, a new one
+#pragma clang fp contract(off)
       constexpr bool masked = decltype(masked_tile)::value;
       constexpr float lift = Matrix<T>::kLift;
       float most[MT];
-      bool moves = false;
+      bool moves = false, beyond = false;
 #pragma unroll
       for (int m = 0; m < MT; ++m) {
-        if constexpr (masked) {
+        if constexpr (masked) {                // (scaled before: a scale of 0 leaves what is not seen out)
 #pragma unroll
           for (int j = 0; j < 8; ++j)
-            if (!(seen[m] >> (16 * (j >> 2) + 4 * of4 + (j & 3)) & 1)) s[m][j >> 2][j & 3] = -INFINITY;
+            s[m][j >> 2][j & 3] = seen[m] >> (16 * (j >> 2) + 4 * of4 + (j & 3)) & 1 ? s[m][j >> 2][j & 3] * a.scale2 : -INFINITY;
         }
         const f32x4 x = s[m][0], y = s[m][1];
-        most[m] = max3(max3(x[0], x[1], x[2]), max3(x[3], y[0], y[1]), max3(y[2], y[3], y[3])) * a.scale2;
-        moves |= most[m] > top[m] + (lift + 8.f);
+        most[m] = max3(max3(x[0], x[1], x[2]), max3(x[3], y[0], y[1]), max3(y[2], y[3], y[3])) * (masked ? 1.f : a.scale2);
+        moves |= most[m] - top[m] > lift + 8.f;
       }
       if (__any(moves)) {
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
           most[m] = fmaxf(most[m], __shfl_xor(most[m], 16));
           most[m] = fmaxf(most[m], __shfl_xor(most[m], 32));
-          const float now = most[m] > top[m] + (lift + 8.f) ? most[m] - lift : top[m];
+          const float now = most[m] - top[m] > lift + 8.f ? most[m] - lift : top[m];
+          if (!masked) beyond |= fabsf(now) > kFar && now != -INFINITY;
           const float back = now == top[m] ? 1.f : __builtin_amdgcn_exp2f(top[m] - now);
           top[m] = now;
           sum[m] *= back;
@@ -423,12 +433,15 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
             if (MT > 1 && n % 2) __builtin_amdgcn_sched_barrier(0);    // few of them out of the accumulation registers at a time
           }
         }
+        if (!masked) far |= __any(beyond) != 0;
       }
     };
-    auto exponentials = [&](int m, int k) {    // the k-th pair of keys of rows m
-      const float ref = top[m] == -INFINITY ? 0.f : top[m];
-      const float one = __builtin_amdgcn_exp2f(fmaf(s[m][k >> 1][2 * (k & 1)], a.scale2, -ref));
-      const float two = __builtin_amdgcn_exp2f(fmaf(s[m][k >> 1][2 * (k & 1) + 1], a.scale2, -ref));
+    auto exponentials = [&](auto masked_tile, int m, int k) {  // the k-th pair of keys of rows m
+#pragma clang fp contract(off)
+      constexpr bool masked = decltype(masked_tile)::value;
+      const float ref = top[m] == -INFINITY ? 0.f : top[m], x = s[m][k >> 1][2 * (k & 1)], y = s[m][k >> 1][2 * (k & 1) + 1];
+      const float one = __builtin_amdgcn_exp2f(masked ? x - ref : fmaf(x, a.scale2, -ref));
+      const float two = __builtin_amdgcn_exp2f(masked ? y - ref : fmaf(y, a.scale2, -ref));
       sum[m] += one + two;
       p[m][k] = pack<T>(one, two);
     };
@@ -445,7 +458,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
           output(m, n);
           if (m + 1 < MT) {
 #pragma unroll
-            for (int k = n * 4 / E; k < (n + 1) * 4 / E; ++k) exponentials(m + 1, k);
+            for (int k = n * 4 / E; k < (n + 1) * 4 / E; ++k) exponentials(std::false_type(), m + 1, k);
           }
         }
     };
@@ -595,7 +608,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
 #pragma unroll
               for (int m = 0; m < MT; ++m)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) exponentials(m, k);
+                for (int k = 0; k < 4; ++k) exponentials(std::false_type(), m, k);
 #pragma unroll
               for (int m = 0; m < MT; ++m)
 #pragma unroll
@@ -630,7 +643,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
         load_keys(following, next0, next1, more ? k_lane : 0);
         references(std::false_type(), 0);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) exponentials(0, k);
+        for (int k = 0; k < 4; ++k) exponentials(std::false_type(), 0, k);
 #pragma unroll
         for (int k = 0; k < 4 * E; ++k) transpose(k);
         __builtin_amdgcn_sched_barrier(0);
@@ -645,6 +658,11 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
       }
     }
     // the last cached keys, the new ones, and what lies on and behind pages that are not there
+    if (far) {
+      nothing();
+      t = now.t0 + key_wave;
+      load_tile(t);
+    }
     while (t < t1) {
       const int key0 = t * kTile, me = thread(), row16 = me & 15, of4 = me >> 4 & 3;
       scores();
@@ -687,7 +705,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
 #pragma unroll
       for (int m = 0; m < MT; ++m)
 #pragma unroll
-        for (int k = 0; k < 4; ++k) exponentials(m, k);
+        for (int k = 0; k < 4; ++k) exponentials(std::true_type(), m, k);
       {
         // Infinities and NaN among the values: 0 * inf would reach rows that do not see the key.  Such a key is taken out of
         // the matrix product and added by the rows that see it.

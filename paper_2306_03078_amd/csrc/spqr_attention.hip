@@ -1,9 +1,6 @@
 // Softmax attention of a step's rows over a paged cache: checks and launch plan (kernels: spqr_attention.h).
 #include "spqr_attention.h"
 
-#include <algorithm>
-#include <limits>
-
 namespace spqr_srv {
 
 #define SPQR_ATTEND_EXTERN(D)                                                                        \
@@ -113,10 +110,7 @@ extern "C" int spqr_tree_attention(const spqr_step_t* s, int32_t layer, const vo
   a.part_ml = a.part_o + 2ll * p.workgroups * a.chunk_rows * s->head_dim;
   a.requests = s->requests; a.tokens = s->tokens; a.kv_heads = s->kv_heads; a.group = s->heads / s->kv_heads;
   a.log_page = __builtin_ctz(s->page); a.pages = s->pages; a.max_pages = s->max_pages; a.words = s->mask_words;
-  // What a row does not see is -inf before the scale, and 0 * inf is no number that keeps it out: a scale of 0 is the smallest number there
-  // is, with which scores of binary32 are below 2^-20.  (Queries taken as 0 by a mask of their bits instead: heads of 256, 512 rows
-  // and more, 5 to 8 % slower.)
-  a.scale2 = std::max(scale2, std::numeric_limits<float>::denorm_min());
+  a.scale2 = scale2;
   a.turn = s->scale < 0.f ? 0x80008000u : 0u;
   a.inv_group = 1.0f / (float)a.group;
   a.workgroups = p.workgroups;
