@@ -477,7 +477,7 @@ __global__ void __launch_bounds__(KW == 1 ? 512 : 256) attend_kernel(Attend a) {
       // is full.
       // Measured against four wavefronts of 64 rows that each load every tile (KW = 4's way): 512 rows, 8 heads of 128 over up to
       // 32000 keys, 4 requests 142 -> 132 us; 4096 rows over 260000 keys of one head 631 -> 580 us (940 TFLOP/s); heads of 64
-      // elements 60 -> 49 us, of 256 194 -> 154 us (where 160 to 190 bytes of a lane's registers do not fit and go to memory).  Dropped, by the first of these: two stages on their way with the
+      // elements 60 -> 49 us, of 256 194 -> 154 us (where 160 to 172 bytes of a lane's registers do not fit and go to memory; of 128: 12).  Dropped, by the first of these: two stages on their way with the
       // queries in LDS, in whose registers they are (12 % slower), priorities around the products (1 %), halves of the wavefronts
       // half a stage apart (8 %), half-full chunks' tiles shared among twice the wavefronts (equal).
       constexpr int kK = (4 * kST * D + 511) / 512, kV = (2 * kST * D + 511) / 512;
