@@ -93,20 +93,17 @@ int32_t spqr_adapter_tiles(int32_t rows, int32_t slots);
  * SPQR_ADAPTER_TILE rows.  Rows of no request (behind q_start[requests]) are in no tile. */
 int spqr_adapter_plan(const spqr_adapter_plan_t* p, void* stream);
 
-/* out_p[t] = y_p[t] + scale[a] * B_p[a] (A_p[a] x[t])  for the `count` projections p that share x, a the slot of row t's tile;
+/* out_p[t] = y_p[t] + scale_p[a] * B_p[a] (A_p[a] x[t])  for the `count` projections p that share x, a the slot of row t's tile;
  * out_p[t] = y_p[t] for rows of no adapter; rows in no tile are not written. */
 typedef struct spqr_adapters_t {
   int32_t count;                 /* 1 .. SPQR_MAX_FUSED                                                                 */
   int32_t width;                 /* elements of a row of x, 1 .. SPQR_MAX_WIDTH                                         */
-  int32_t slots;                 /* the plan's                                                                          */
+  int32_t slots;                 /* 1 .. SPQR_MAX_SLOTS; the plan's                                                     */
   int32_t dtype;                 /* SPQR_F16 or SPQR_BF16: x, A, B                                                      */
   int32_t y_dtype;               /* of y and out                                                                        */
   int32_t m[SPQR_MAX_FUSED];     /* rows of B: elements of a row of y, 1 .. SPQR_MAX_WIDTH                              */
   int32_t max_rank[SPQR_MAX_FUSED];      /* 1 .. SPQR_MAX_RANK                                                          */
-  const void* A[SPQR_MAX_FUSED];         /* [slots][max_rank][width]                                                    */
-  const void* B[SPQR_MAX_FUSED];         /* [slots][m][max_rank]                                                        */
-  const int32_t* rank[SPQR_MAX_FUSED];   /* [slots] 0 .. max_rank (cut to that): what lies behind it in A and B does not
-                                            count, whatever it holds.  NULL: max_rank everywhere                         */
+  const void* bank[SPQR_MAX_FUSED];      /* spqr_adapters_bank_bytes(a, p) bytes, 256-byte aligned, filled by spqr_adapters_pack   */
   const float* scale[SPQR_MAX_FUSED];    /* [slots]; NULL: 1                                                             */
   const void* y[SPQR_MAX_FUSED];         /* [rows][m]; NULL: zero                                                       */
   void* out[SPQR_MAX_FUSED];             /* [rows][m]; may be y (same address and stride), overlaps nothing else        */
@@ -118,14 +115,25 @@ typedef struct spqr_adapters_t {
   int64_t workspace_bytes;
 } spqr_adapters_t;
 
-/* Bytes of scratch that spqr_adapters needs for steps of up to `rows` rows, by count, width and max_rank of the descriptor (no
+/* Bytes of projection p's bank (by count, width, slots, m and max_rank), or a negative status.  Host arithmetic only.  A bank holds its
+ * adapters' weights in the order that the kernels read them, ranks rounded up to 16 (A) and 32 (B, above 16), widths to 128, m to 64. */
+int64_t spqr_adapters_bank_bytes(const spqr_adapters_t* a, int32_t p);
+
+/* Fills `slots` slots of projection p's bank, from slot `first` on, with the adapters A [slots][max_rank][width], B [slots][m][max_rank]
+ * of type a->dtype and rank [slots] (0 .. max_rank, cut to that; NULL: max_rank): what lies behind an adapter's rank in A and B does not
+ * count, whatever it holds.  Of `a` the sizes, dtype and bank[p] are looked at; A, B and rank may go after the call has run.  Slots
+ * that were never filled must not be used by a plan (their ranks are what the memory held: clear it, and they add nothing). */
+int spqr_adapters_pack(const spqr_adapters_t* a, int32_t p, int32_t first, int32_t slots, const void* A, const void* B, const int32_t* rank,
+                       void* stream);
+
+/* Bytes of scratch that spqr_adapters needs for steps of up to `rows` rows, by count, width, slots and max_rank of the descriptor (no
  * pointers are looked at); or a negative status.  Host arithmetic only. */
 int64_t spqr_adapters_workspace_bytes(const spqr_adapters_t* a, int32_t rows);
 
 /* A step's rows through the adapters.  `plan` is one that spqr_adapter_plan filled (earlier on the same stream, or otherwise
  * before it) with the same slots; of its arrays count, tile and row are read.  Sums in binary32; A x meets B as a sum of two
- * (SPQR_F16) or three (SPQR_BF16) values of `dtype`, which hold it to 2^-22 of a row's largest element or better.  x, A and B are finite
- * where they count: an infinity or NaN gives infinities or NaN in its row. */
+ * (SPQR_F16) or three (SPQR_BF16) values of `dtype`, which hold it to 2^-22 of a row's largest element or better.  An infinity or
+ * NaN in a row of x gives infinities or NaN in that row. */
 int spqr_adapters(const spqr_adapters_t* a, const spqr_adapter_plan_t* plan, void* stream);
 
 /* ---- log probabilities --------------------------------------------------------- */

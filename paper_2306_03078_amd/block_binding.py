@@ -35,8 +35,8 @@ class spqr_adapter_plan_t(C.Structure):
 
 class spqr_adapters_t(C.Structure):
     _fields_ = ([(k, _i32) for k in ("count", "width", "slots", "dtype", "y_dtype")]
-                + [(k, t * SPQR_MAX_FUSED) for k, t in (("m", _i32), ("max_rank", _i32), ("A", _vp), ("B", _vp), ("rank", _vp), ("scale", _vp),
-                                                        ("y", _vp), ("out", _vp), ("y_stride", _i64), ("out_stride", _i64))]
+                + [(k, t * SPQR_MAX_FUSED) for k, t in (("m", _i32), ("max_rank", _i32), ("bank", _vp), ("scale", _vp), ("y", _vp),
+                                                         ("out", _vp), ("y_stride", _i64), ("out_stride", _i64))]
                 + [("x", _vp), ("x_stride", _i64), ("workspace", _vp), ("workspace_bytes", _i64)])
 
 
@@ -56,6 +56,8 @@ def _lib():
             f.restype, f.argtypes = C.c_int, [_vp] + rest
             _entry[name] = f if B._call is B._ctypes_call else C.cast(f, _vp).value
         lib.spqr_adapter_tiles.restype, lib.spqr_adapter_tiles.argtypes = _i32, [_i32, _i32]
+        lib.spqr_adapters_bank_bytes.restype, lib.spqr_adapters_bank_bytes.argtypes = _i64, [_vp, _i32]
+        lib.spqr_adapters_pack.restype, lib.spqr_adapters_pack.argtypes = C.c_int, [_vp, _i32, _i32, _i32, _vp, _vp, _vp, _vp]
         lib.spqr_adapters_workspace_bytes.restype, lib.spqr_adapters_workspace_bytes.argtypes = _i64, [_vp, _i32]
         lib.spqr_token_logprobs_workspace_bytes.restype, lib.spqr_token_logprobs_workspace_bytes.argtypes = _i64, [_vp]
     return lib
@@ -207,11 +209,11 @@ def spqr_adapter_plan(plan: SpQRAdapterPlan, adapter, q_start=None, stream=None)
 
 
 class SpQRAdapters:
-    """Banks of low-rank adapters for projections that share their input: A[p] [slots, max_rank, width], B[p] [slots, m, max_rank], all
-    float16 or all bfloat16 (max_rank and m may differ from projection to projection).  rank, scale: int32 and float32 [slots], one
-    for all projections, a list of one each, or None (max_rank and 1).  rows: of the largest step, which the scratch is made for;
-    workspace: a device tensor to use instead (banks that are called one after the other may share it).  Slots may be refilled
-    between calls."""
+    """Banks of low-rank adapters for projections that share their input, packed from A[p] [slots, max_rank, width] and B[p] [slots, m,
+    max_rank], all float16 or all bfloat16 (max_rank and m may differ from projection to projection; A and B are not needed
+    afterwards).  rank: int32 [slots], one for all projections, a list of one each, or None (max_rank).  scale: the same, float32
+    [slots], read by each call; None: 1.  rows: of the largest step, which the scratch is made for; workspace: a device tensor to use instead
+    (banks that are called one after the other may share it)."""
 
     def __init__(self, A, B, rank=None, scale=None, *, rows, workspace=None):
         import torch
@@ -222,27 +224,28 @@ class SpQRAdapters:
             raise ValueError(f"as many A as B, 1 to {SPQR_MAX_FUSED}")
         d = self.desc = spqr_adapters_t()
         self.device, self.dtype, self.rows = A[0].device, A[0].dtype, int(rows)
-        if self.device.type != "cuda" or self.dtype not in (torch.float16, torch.bfloat16) or A[0].dim() != 3:
-            raise ValueError("A: float16 or bfloat16 device tensors [slots, max_rank, width]")
+        if self.device.type != "cuda" or self.dtype not in (torch.float16, torch.bfloat16) or any(t.dim() != 3 for t in A + B):
+            raise ValueError("A, B: float16 or bfloat16 device tensors [slots, max_rank, width], [slots, m, max_rank]")
         self._index = self.device.index
         self.slots, self.width = A[0].shape[0], A[0].shape[2]
-        rank, scale = ([v] * k if v is None or hasattr(v, "dtype") else list(v) for v in (rank, scale))
-        if len(rank) != k or len(scale) != k:
-            raise ValueError(f"rank, scale: one, or {k}")
-        self.m = []
-        for p, (a, b) in enumerate(zip(A, B)):
-            for t, name, shape in ((a, "A", (self.slots, a.shape[1] if a.dim() == 3 else -1, self.width)),
-                                   (b, "B", (self.slots, b.shape[1] if b.dim() == 3 else -1, a.shape[1] if a.dim() == 3 else -1))):
-                if t.dtype != self.dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
-                    raise ValueError(f"{name}[{p}]: a contiguous {self.dtype} tensor {list(shape)} on {self.device}, not {t.dtype} {list(t.shape)} on {t.device}")
-            for t, name, dtype in ((rank[p], "rank", torch.int32), (scale[p], "scale", torch.float32)):
-                if t is not None and (t.dtype != dtype or tuple(t.shape) != (self.slots,) or not t.is_contiguous() or t.device != self.device):
-                    raise ValueError(f"{name}: a contiguous {dtype} tensor [{self.slots}] on {self.device}")
-            d.max_rank[p], d.m[p], d.A[p], d.B[p] = a.shape[1], b.shape[1], a.data_ptr(), b.data_ptr()
-            d.rank[p], d.scale[p] = (None if t is None else t.data_ptr() for t in (rank[p], scale[p]))
-            self.m.append(b.shape[1])
-        self._kept = A, B, rank, scale
+        self.m, self.max_rank = [b.shape[1] for b in B], [a.shape[1] for a in A]
+        scale = [scale] * k if scale is None or hasattr(scale, "dtype") else list(scale)
+        if len(scale) != k:
+            raise ValueError(f"scale: one, or {k}")
+        for t in scale:
+            if t is not None and (t.dtype != torch.float32 or tuple(t.shape) != (self.slots,) or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"scale: a contiguous float32 tensor [{self.slots}] on {self.device}")
+        self.scale = scale
         d.count, d.width, d.slots, d.dtype = k, self.width, self.slots, S._dtypes[self.dtype]
+        for p in range(k):
+            d.max_rank[p], d.m[p], d.scale[p] = self.max_rank[p], self.m[p], None if scale[p] is None else scale[p].data_ptr()
+        self.banks = []
+        for p in range(k):
+            need = int(lib.spqr_adapters_bank_bytes(C.byref(d), p))
+            if need < 0:
+                raise SpQRError(need, "spqr_adapters_bank_bytes")
+            self.banks.append(torch.empty(need, dtype=torch.uint8, device=self.device))
+            d.bank[p] = self.banks[p].data_ptr()
         need = int(lib.spqr_adapters_workspace_bytes(C.byref(d), self.rows))
         if need < 0:
             raise SpQRError(need, "spqr_adapters_workspace_bytes")
@@ -252,6 +255,32 @@ class SpQRAdapters:
             raise ValueError(f"workspace: a contiguous tensor on {self.device}")
         self.workspace = workspace
         d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
+        self.load(0, A, B, rank)
+
+    def load(self, first, A, B, rank=None, stream=None):
+        """Other adapters into the slots from `first` on: A, B and rank as above, of as many slots as are to be filled."""
+        import torch
+        k, A, B = len(self.m), list(A), list(B)
+        rank = [rank] * k if rank is None or hasattr(rank, "dtype") else list(rank)
+        if len(A) != k or len(B) != k or len(rank) != k:
+            raise ValueError(f"A, B: {k} tensors; rank: one, or {k}")
+        slots = A[0].shape[0]
+        if first < 0 or first + slots > self.slots:
+            raise ValueError(f"slots {first} .. {first + slots - 1} of {self.slots}")
+        for p in range(k):
+            for t, name, shape in ((A[p], "A", (slots, self.max_rank[p], self.width)), (B[p], "B", (slots, self.m[p], self.max_rank[p]))):
+                if t.dtype != self.dtype or tuple(t.shape) != shape or not t.is_contiguous() or t.device != self.device:
+                    raise ValueError(f"{name}[{p}]: a contiguous {self.dtype} tensor {list(shape)} on {self.device}, not {t.dtype} {list(t.shape)} on {t.device}")
+            t = rank[p]
+            if t is not None and (t.dtype != torch.int32 or tuple(t.shape) != (slots,) or not t.is_contiguous() or t.device != self.device):
+                raise ValueError(f"rank: a contiguous int32 tensor [{slots}] on {self.device}")
+        lib = _lib()
+        with torch.cuda.device(self._index):
+            to = S._raw_stream(self._index) if stream is None else stream.cuda_stream
+            for p in range(k):
+                rc = lib.spqr_adapters_pack(C.byref(self.desc), p, first, slots, A[p].data_ptr(), B[p].data_ptr(), None if rank[p] is None else rank[p].data_ptr(), to)
+                if rc != 0:
+                    raise SpQRError(int(rc), "spqr_adapters_pack")
 
 
 def spqr_adapters(bank: SpQRAdapters, plan: SpQRAdapterPlan, x, ys=None, outs=None, stream=None):

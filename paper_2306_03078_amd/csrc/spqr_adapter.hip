@@ -85,21 +85,22 @@ __global__ void __launch_bounds__(256) adapter_plan_kernel(spqr_adapter_plan_t p
 // ---------------------------------------------------------------------------------------------------------------------
 // The adapters.
 // ---------------------------------------------------------------------------------------------------------------------
-__device__ __forceinline__ int tile_of(const spqr_adapter_plan_t& plan, const spqr_adapters_t& a, int t, int* rows) {
-  const int slot = plan.tile[2 * t];
-  *rows = min(max(plan.tile[2 * t + 1], 0), kTile);
-  return slot >= 0 && slot < a.slots ? slot : -1;
-}
-__device__ __forceinline__ int rank_of(const spqr_adapters_t& a, int p, int slot) {
-  return a.rank[p] ? min(max(a.rank[p][slot], 0), a.max_rank[p]) : a.max_rank[p];
-}
-
+// Both products run on 16 x 16 x 32 matrix instructions.  An operand's lane l holds 8 values of line l & 15, so neighbouring lanes hold different
+// lines, and loads of rows as they lie take a trip through the address unit for each lane (64 a load in place of 16: A x and B (A x) of 5000 rows
+// were bound by it, 60 and 230 us).  A bank's weights are therefore packed, once, as operands: 64 lanes x 16 bytes one after the other, zeros
+// where there is no weight.
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename T> struct __attribute__((packed, aligned(sizeof(T)))) Run4 { T e[4]; };
 template <typename T> using x8 = T __attribute__((ext_vector_type(8)));
 
 __device__ __forceinline__ f32x4 mfma(x8<_Float16> a, x8<_Float16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_f16(a, b, c, 0, 0, 0); }
 __device__ __forceinline__ f32x4 mfma(x8<__bf16> a, x8<__bf16> b, f32x4 c) { return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0); }
+
+// What is the same for all threads, by way of the scalar cache: such loads wait for nothing but each other.
+template <typename V>
+__device__ __forceinline__ V uniform(const V* p) {
+  return *(const __attribute__((address_space(4))) V*)(uintptr_t)p;
+}
 
 // Eight neighbouring elements of a row of n from k on, zeros behind its end.
 template <typename T>
@@ -116,325 +117,565 @@ __device__ __forceinline__ x8<T> operand_to(const T* row, int k, int n) {
   return v;
 }
 
-constexpr int kGroup = 64;                       // ranks that a workgroup takes at once
-constexpr int kUnit = 64;                        // elements of a row of x that a wavefront takes at once: two products, 128 bytes of a row
-constexpr int kMostSplits = 16;
+// A projection's bank: the slots' ranks (rounded up to 256 bytes), then slot after slot
+//   A: [tile of 16 ranks][step of 32 elements of x]: lane l has rank 16 * tile + (l & 15), elements 32 * step + 8 * (l >> 4) ..
+//   B: [32 ranks][64 m][4: j]: lane l has m = 64 * block + 4 * (l & 15) + j, ranks 32 * h + 8 * (l >> 4) .. -- of the four results of a lane, those of j
+//      0 .. 3 are neighbours, and neighbouring lanes' too.  Up to 16 ranks: [64 m][2]: lanes below 32 are the first half of j = 2 i, the others of
+//      j = 2 i + 1.
+struct Bank {
+  int tiles, steps;                              // of 16 ranks; of 32 elements of x, a multiple of 4
+  int halves, blocks;                            // of 32 ranks, 0: up to 16 ranks; of 64 m
+  __host__ __device__ Bank(int width, int m, int max_rank)
+      : tiles((max_rank + 15) / 16), steps((width + 127) / 128 * 4), halves(max_rank <= 16 ? 0 : (max_rank + 31) / 32), blocks((m + 63) / 64) {}
+  __host__ __device__ int64_t a_operands() const { return (int64_t)tiles * steps; }
+  __host__ __device__ int64_t operands() const { return a_operands() + (int64_t)blocks * (halves == 0 ? 2 : 4 * halves); }
+};
+__host__ __device__ inline int64_t header_bytes(int slots) { return ((int64_t)slots * 4 + 255) / 256 * 256; }
+
+struct Pack {
+  const uint16_t *A, *B;
+  const int32_t* rank;
+  uint8_t* bank;
+  int width, m, max_rank, slots, first;
+};
+
+// A thread a lane of an operand.
+__global__ void __launch_bounds__(256) pack_kernel(Pack a) {
+  const Bank bank(a.width, a.m, a.max_rank);
+  const int slot = blockIdx.y;                   // of those that are given
+  const int rank = a.rank ? min(max(a.rank[slot], 0), a.max_rank) : a.max_rank;
+  if (blockIdx.x == 0 && threadIdx.x == 0) reinterpret_cast<int32_t*>(a.bank)[a.first + slot] = rank;
+  u32x4* to = reinterpret_cast<u32x4*>(a.bank + header_bytes(a.slots)) + (a.first + slot) * bank.operands() * 64;
+  const uint16_t *A = a.A + (int64_t)slot * a.max_rank * a.width, *B = a.B + (int64_t)slot * a.m * a.max_rank;
+  for (int64_t i = blockIdx.x * 256ll + threadIdx.x; i < bank.operands() * 64; i += gridDim.x * 256ll) {
+    const int64_t which = i / 64;
+    const int lane = (int)(i % 64), l16 = lane & 15, g = lane >> 4;
+    uint16_t v[8];
+    if (which < bank.a_operands()) {
+      const int k = (int)(which / bank.steps) * 16 + l16, at = (int)(which % bank.steps) * 32 + 8 * g;
+      for (int e = 0; e < 8; ++e) v[e] = k < rank && at + e < a.width ? A[(int64_t)k * a.width + at + e] : 0;
+    } else {
+      const int64_t w = which - bank.a_operands();
+      int m, k;
+      if (bank.halves == 0) {
+        m = (int)(w / 2) * 64 + 4 * l16 + 2 * (int)(w % 2) + (g >> 1);
+        k = 8 * (g & 1);
+      } else {
+        m = (int)(w / 4 % bank.blocks) * 64 + 4 * l16 + (int)(w % 4);
+        k = (int)(w / 4 / bank.blocks) * 32 + 8 * g;
+      }
+      for (int e = 0; e < 8; ++e) v[e] = m < a.m && k + e < rank ? B[(int64_t)m * a.max_rank + k + e] : 0;
+    }
+    u32x4 x;
+    for (int e = 0; e < 4; ++e) x[e] = v[2 * e] | (uint32_t)v[2 * e + 1] << 16;
+    to[i] = x;
+  }
+}
+
+constexpr int kStage = 128;                      // elements of x at a time
+constexpr int kMostSplits = 8;
 constexpr int kShrinkGroups = 512;               // workgroups that A x is split into where tiles are few
+constexpr int kExpandGroups = 768, kMostRounds = 4;
+constexpr int kWaveTiles = 4;                    // tiles of 16 ranks that a wavefront takes at once
 
 // How a call is cut: into how many parts the sum over the elements of x, for the tiles that there are (no fewer than the step's rows may
 // have, which the workspace is made for).
 struct Cut {
-  int groups;                                    // of up to 64 ranks, of all projections
-  int units;                                     // of the elements of x
-  int total;                                     // floats of a row of A x: ranks rounded up to 16
+  int rank_tiles;                                // of 16 ranks, of all projections
+  int rank_halves;                               // of 32 ranks, of all projections: blocks of A x
+  int stages;                                    // of the elements of x
   __host__ __device__ int splits(int there, int rows) const {
     const int full = (rows + kTile - 1) / kTile, tiles = there > full ? there : full;
-    const int by_work = kShrinkGroups / (tiles * groups > 0 ? tiles * groups : 1), by_units = (units + 3) / 4;
-    const int s = by_work < by_units ? by_work : by_units;
+    const int groups = (rank_tiles + 4 * kWaveTiles - 1) / (4 * kWaveTiles);
+    const int by_work = kShrinkGroups / (tiles * groups > 0 ? tiles * groups : 1), by_stages = (stages + 3) / 4;
+    const int s = by_work < by_stages ? by_work : by_stages;
     return s < 1 ? 1 : s < kMostSplits ? s : kMostSplits;
   }
 };
-__host__ __device__ inline int padded(int rank) { return (rank + 15) / 16 * 16; }
 
-// v[split][row][offset of p + k] = the split's part of A_p[slot][k] . x[row], NR * 16 ranks of up to NS * 16 rows: 16 ranks x 32 elements
-// times 32 elements x 16 rows a product, operands straight from memory.  The workgroup's wavefronts take units in turn and add up in LDS.
+// A call as the kernels take it: what a workgroup needs of a projection lies together.
+struct Projection {
+  const uint8_t* bank;
+  const float* scale;
+  const void* y;
+  void* out;
+  int64_t y_stride, out_stride;
+  int m, max_rank;
+  int at;                                        // its first block of 32 ranks of A x
+};
+struct Call {
+  Projection p[SPQR_MAX_FUSED];
+  const void* x;
+  int64_t x_stride;
+  const int32_t *count, *tile, *row;
+  float* v;                                      // A x: [splits][tiles][blocks of 32 ranks][16 rows: 4][lane][8], as the operands of the next product
+  Cut cut;
+  int width, slots, rows, max_tiles, v_tiles;
+  int span;                                      // elements of the outputs' rows that a workgroup takes
+  int rank_tile[SPQR_MAX_FUSED * SPQR_MAX_RANK / 16];      // projection + 256 * its tile of 16 ranks
+};
+__device__ __forceinline__ float* v_of(const Call& c, int split, int tile, int half, int sub) {
+  return c.v + (((int64_t)split * c.v_tiles + tile) * c.cut.rank_halves + half) * (4 * 512) + sub * 512;
+}
+
+// A tile as the kernels take it: slot -1 where no adapter (or none that the bank has) is used; rows, 0 behind the last tile; row: a lane's
+// of them, -1 where there is none; count: of all tiles.
+struct Tile { int slot, rows, count, row; };
+
+__device__ __forceinline__ Tile tile_at(const Call& c, int t) {
+  const int in_tile = threadIdx.x & (kTile - 1), row = c.row[(int64_t)t * kTile + in_tile];
+  const int count = min(uniform(c.count), c.max_tiles), slot = uniform(c.tile + 2 * t), rows = uniform(c.tile + 2 * t + 1);
+  Tile v;
+  v.count = count;
+  v.slot = slot >= 0 && slot < c.slots ? slot : -1;
+  v.rows = t < count ? min(max(rows, 0), kTile) : 0;
+  v.row = in_tile < v.rows && row >= 0 && row < c.rows ? row : -1;
+  return v;
+}
+__device__ __forceinline__ int rank_of(const Projection& p, int slot) {
+  return slot < 0 ? 0 : min(max(uniform(reinterpret_cast<const int32_t*>(p.bank) + slot), 0), p.max_rank);
+}
+template <typename T>
+__device__ __forceinline__ const x8<T>* slot_of(const Call& c, const Projection& p, int slot) {
+  return reinterpret_cast<const x8<T>*>(p.bank + header_bytes(c.slots)) + slot * Bank(c.width, p.m, p.max_rank).operands() * 64;
+}
+
+// 16 ranks of 16 rows to where the next product finds them: lane (row, 4 * g ..) of tile `tile` of the projection.
+__device__ __forceinline__ void put(const Call& c, const Projection& p, int split, int t, int tile, int sub, int lane, f32x4 sum) {
+  const int k = 16 * (tile & 1) + 4 * (lane >> 4);         // of the 32 ranks
+  *reinterpret_cast<f32x4*>(v_of(c, split, t, p.at + tile / 2, sub) + ((k >> 3) * 16 + (lane & 15)) * 8 + (k & 7)) = sum;
+}
+
+// Up to 16 rows: NR tiles of 16 ranks of one projection, the workgroup's wavefronts take stages of 128 elements in turn and add up in LDS.  x comes
+// straight from memory: few rows are few addresses.
+template <typename T, int NR>
+__device__ __forceinline__ void shrink_few(const Call& c, const Tile& t, const Projection& p, int tile0, int tiles, int split, int s0, int s1, f32x4* red) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4, n = c.width;
+  const int steps = (n + 127) / 128 * 4;
+  const x8<T>* A = slot_of<T>(c, p, t.slot) + (int64_t)tile0 * steps * 64 + lane;
+  const T* x = static_cast<const T*>(c.x) + max(__shfl(t.row, min(l16, t.rows - 1)), 0) * c.x_stride;
+  f32x4 acc[NR];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) acc[r] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto add = [&](auto load, int s) {
+    x8<T> a[4][NR], b[4];
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+#pragma unroll
+      for (int r = 0; r < NR; ++r) a[h][r] = A[((int64_t)min(r, tiles - 1) * steps + 4 * s + h) * 64];
+      b[h] = load(kStage * s + 32 * h + 8 * g);
+    }
+#pragma unroll
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) acc[r] = mfma(a[h][r], b[h], acc[r]);
+  };
+  const int last = min(s1, n / kStage);
+  int s = s0 + wave;
+  for (; s < last; s += 4) add([&](int k) { return operand(x, k); }, s);
+  if (s < s1) add([&](int k) { return operand_to(x, k, n); }, s);
+#pragma unroll
+  for (int r = 0; r < NR; ++r) red[(wave * NR + r) * 64 + lane] = acc[r];
+  __syncthreads();
+  for (int r = wave; r < tiles && r < NR; r += 4) {
+    f32x4 sum = red[r * 64 + lane];
+    for (int w = 1; w < 4; ++w) sum += red[(w * NR + r) * 64 + lane];
+    put(c, p, split, blockIdx.y, tile0 + r, 0, lane, sum);
+  }
+}
+
+// More rows: NS * 16 of them through LDS, a stage at a time (rows of 256 bytes, 16-byte pieces turned by the row so that 16 rows' are in all banks);
+// each wavefront has NR tiles of 16 ranks of its own, of any projections.
 template <typename T, int NR, int NS>
-__device__ __forceinline__ void shrink_tile(const T* A, int64_t a_stride, int ranks, const T* x, int64_t x_stride, int n, const int32_t* row, int rows,
-                                            int u0, int u1, float* v, int total, f32x4* red) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, l16 = lane & 15, g = lane >> 4;
-  const T *ap[NR], *xp[NS];
-  int64_t at[NS];
+__device__ __forceinline__ void shrink_many(const Call& c, const Tile& t, int first, int split, int s0, int s1, x8<T>* xs) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, n = c.width;
+  const int steps = (n + 127) / 128 * 4;
+  // a thread's piece of NS rows
+  const int piece = tid & 15, row0 = tid >> 4;
+  const T* x[NS];
 #pragma unroll
-  for (int r = 0; r < NR; ++r) ap[r] = A + min(16 * r + l16, ranks - 1) * a_stride;
+  for (int i = 0; i < NS; ++i) x[i] = static_cast<const T*>(c.x) + max(__shfl(t.row, 16 * i + row0), 0) * c.x_stride + 8 * piece;
+  // a wavefront's tiles; one that is none reads those of the first
+  const x8<T>* A[NR];
+  bool there[NR];
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    at[s] = row[min(16 * s + l16, rows - 1)];
-    xp[s] = x + at[s] * x_stride;
+  for (int r = 0; r < NR; ++r) {
+    const int i = first + wave + 4 * r, of = c.rank_tile[i < c.cut.rank_tiles ? i : first];
+    const Projection& p = c.p[of & 255];
+    there[r] = i < c.cut.rank_tiles && 16 * (of >> 8) < rank_of(p, t.slot);
+    A[r] = slot_of<T>(c, p, t.slot) + (int64_t)(of >> 8) * steps * 64 + lane;
   }
   f32x4 acc[NR][NS];
 #pragma unroll
   for (int r = 0; r < NR; ++r)
 #pragma unroll
-    for (int s = 0; s < NS; ++s) acc[r][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-  auto add = [&](auto load, int u) {
-    x8<T> a[2][NR], b[2][NS];
+    for (int i = 0; i < NS; ++i) acc[r][i] = f32x4{0.f, 0.f, 0.f, 0.f};
+  x8<T> next[NS];
+  auto load_x = [&](int s) {
+    if (kStage * (s + 1) <= n) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = kUnit * u + 32 * h + 8 * g;
+      for (int i = 0; i < NS; ++i) next[i] = operand(x[i], kStage * s);
+    } else {
 #pragma unroll
-      for (int r = 0; r < NR; ++r) a[h][r] = load(ap[r], k);
-#pragma unroll
-      for (int s = 0; s < NS; ++s) b[h][s] = load(xp[s], k);
+      for (int i = 0; i < NS; ++i) next[i] = operand_to(x[i], kStage * s, n - 8 * piece);
     }
+  };
+  load_x(s0);
+  for (int s = s0; s < s1; ++s) {
+    x8<T> a[4][NR];
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < 4; ++h)
+#pragma unroll
+      for (int r = 0; r < NR; ++r) a[h][r] = A[r][(4 * s + h) * 64];
+    x8<T>* buffer = xs + ((s - s0) & 1) * (NS * 256);
+#pragma unroll
+    for (int i = 0; i < NS; ++i) buffer[(16 * i + row0) * 16 + (piece ^ row0)] = next[i];
+    if (s + 1 < s1) load_x(s + 1);
+    __syncthreads();
+#pragma unroll
+    for (int h = 0; h < 4; ++h) {
+      x8<T> b[NS];
+#pragma unroll
+      for (int i = 0; i < NS; ++i) b[i] = buffer[(16 * i + l16) * 16 + ((4 * h + g) ^ l16)];
 #pragma unroll
       for (int r = 0; r < NR; ++r)
 #pragma unroll
-        for (int s = 0; s < NS; ++s) acc[r][s] = mfma(a[h][r], b[h][s], acc[r][s]);
-  };
-  int u = u0 + wave;
-  for (; u < u1 && kUnit * (u + 1) <= n; u += 4) add([](const T* p, int k) { return operand(p, k); }, u);
-  for (; u < u1; u += 4) add([&](const T* p, int k) { return operand_to(p, k, n); }, u);
+        for (int i = 0; i < NS; ++i) acc[r][i] = mfma(a[h][r], b[i], acc[r][i]);
+    }
+  }
 #pragma unroll
   for (int r = 0; r < NR; ++r)
+    if (there[r]) {
+      const int of = c.rank_tile[first + wave + 4 * r];
 #pragma unroll
-    for (int s = 0; s < NS; ++s) red[(wave * NR * NS + r * NS + s) * 64 + lane] = acc[r][s];
-  __syncthreads();
-  for (int i = wave; i < NR * NS; i += 4) {
-    const int r = i / NS, s = i % NS;
-    f32x4 sum = red[i * 64 + lane];
-    for (int w = 1; w < 4; ++w) sum += red[(w * NR * NS + i) * 64 + lane];
-    const int token = 16 * s + l16;
-    if (token < rows && 16 * r < ranks) *reinterpret_cast<f32x4*>(v + (int64_t)row[token] * total + 16 * r + 4 * g) = sum;
-  }
-  __syncthreads();
-}
-
-template <typename T, int NR>
-__device__ __forceinline__ void shrink_rows(const T* A, int64_t a_stride, int ranks, const T* x, int64_t x_stride, int n, const int32_t* row, int rows,
-                                            int u0, int u1, float* v, int total, f32x4* red) {
-  if (rows <= 16) shrink_tile<T, NR, 1>(A, a_stride, ranks, x, x_stride, n, row, rows, u0, u1, v, total, red);
-  else if (rows <= 32) shrink_tile<T, NR, 2>(A, a_stride, ranks, x, x_stride, n, row, rows, u0, u1, v, total, red);
-  else shrink_tile<T, NR, 4>(A, a_stride, ranks, x, x_stride, n, row, rows, u0, u1, v, total, red);
-}
-
-// The tile's rows into LDS; entries that are no rows of the step end it.
-__device__ __forceinline__ int rows_of_tile(const spqr_adapter_plan_t& plan, int t, int rows, int32_t* row) {
-  if (threadIdx.x < kTile) row[threadIdx.x] = plan.row[(int64_t)t * kTile + threadIdx.x];
-  __syncthreads();
-  const int bad = threadIdx.x < rows && (row[threadIdx.x & (kTile - 1)] < 0 || row[threadIdx.x & (kTile - 1)] >= plan.rows);
-  return __syncthreads_or(bad) ? 0 : rows;
+      for (int i = 0; i < NS; ++i) put(c, c.p[of & 255], split, blockIdx.y, of >> 8, i, lane, acc[r][i]);
+    }
 }
 
 template <typename T>
-__global__ void __launch_bounds__(256) shrink_kernel(spqr_adapters_t a, spqr_adapter_plan_t plan, Cut cut, float* v) {
-  __shared__ f32x4 red[4 * 16 * 64];
-  __shared__ int32_t row[kTile];
-  const int tiles = min(plan.count[0], plan.max_tiles), splits = cut.splits(tiles, plan.rows);
-  const int64_t items = (int64_t)tiles * cut.groups * splits;
-  for (int64_t i = blockIdx.x; i < items; i += gridDim.x) {
-    const int group = (int)(i % cut.groups), t = (int)(i / cut.groups % tiles), split = (int)(i / cut.groups / tiles);
-    int rows, p = 0, g = group, at = 0;
-    const int slot = tile_of(plan, a, t, &rows);
-    for (; g >= (a.max_rank[p] + kGroup - 1) / kGroup; ++p) { g -= (a.max_rank[p] + kGroup - 1) / kGroup; at += padded(a.max_rank[p]); }
-    const int ranks = slot < 0 ? 0 : min(rank_of(a, p, slot) - kGroup * g, kGroup);
-    if (ranks <= 0) continue;
-    rows = rows_of_tile(plan, t, rows, row);
-    if (rows == 0) continue;
-    const T* A = static_cast<const T*>(a.A[p]) + ((int64_t)slot * a.max_rank[p] + kGroup * g) * a.width;
-    const T* x = static_cast<const T*>(a.x);
-    float* to = v + (int64_t)split * plan.rows * cut.total + at + kGroup * g;
-    const int u0 = (int)((int64_t)cut.units * split / splits), u1 = (int)((int64_t)cut.units * (split + 1) / splits);
-    if (ranks <= 16) shrink_rows<T, 1>(A, a.width, ranks, x, a.x_stride, a.width, row, rows, u0, u1, to, cut.total, red);
-    else if (ranks <= 32) shrink_rows<T, 2>(A, a.width, ranks, x, a.x_stride, a.width, row, rows, u0, u1, to, cut.total, red);
-    else shrink_rows<T, 4>(A, a.width, ranks, x, a.x_stride, a.width, row, rows, u0, u1, to, cut.total, red);
+__global__ void __launch_bounds__(256) shrink_kernel(Call c) {
+  __shared__ x8<T> shared[2 * 4 * 256];          // two stages of 64 rows; or the wavefronts' sums
+  const Tile t = tile_at(c, blockIdx.y);
+  const int split = (int)blockIdx.x, splits = c.cut.splits(t.count, c.rows);
+  if (t.rows == 0 || t.slot < 0 || split >= splits) return;
+  const int s0 = c.cut.stages * split / splits, s1 = c.cut.stages * (split + 1) / splits;
+  if (t.rows <= 16) {
+    // a workgroup a projection's next tiles: blockIdx.z counts tiles by four, projection by projection
+    int p = 0, z = (int)blockIdx.z;
+    for (; p < SPQR_MAX_FUSED && z >= (c.p[p].max_rank + 16 * kWaveTiles - 1) / (16 * kWaveTiles); ++p) z -= (c.p[p].max_rank + 16 * kWaveTiles - 1) / (16 * kWaveTiles);
+    if (p == SPQR_MAX_FUSED) return;
+    const int tiles = (rank_of(c.p[p], t.slot) + 15) / 16 - kWaveTiles * z;
+    f32x4* red = reinterpret_cast<f32x4*>(shared);
+    if (tiles <= 0) return;
+    if (tiles == 1) shrink_few<T, 1>(c, t, c.p[p], kWaveTiles * z, tiles, split, s0, s1, red);
+    else if (tiles == 2) shrink_few<T, 2>(c, t, c.p[p], kWaveTiles * z, tiles, split, s0, s1, red);
+    else shrink_few<T, 4>(c, t, c.p[p], kWaveTiles * z, tiles, split, s0, s1, red);
+    return;
   }
+  const int first = 4 * kWaveTiles * (int)blockIdx.z, left = c.cut.rank_tiles - first;
+  if (left <= 0) return;
+#define SPQR_SHRINK(NR) do { if (t.rows <= 32) shrink_many<T, NR, 2>(c, t, first, split, s0, s1, shared); else shrink_many<T, NR, 4>(c, t, first, split, s0, s1, shared); } while (0)
+  if (left <= 4) SPQR_SHRINK(1);
+  else if (left <= 8) SPQR_SHRINK(2);
+  else SPQR_SHRINK(4);
+#undef SPQR_SHRINK
 }
 
-// A x as it meets B: v = the sum of PARTS values of 16 bits.  Binary16 holds 22 bits in two, with the row's largest element brought to 2^13
-// .. 2^14, so that what is 2^-27 of it still has its bits and none overflows; bfloat16 24 bits in three, at any size.
+// A x as it meets B: v = the sum of N values of 16 bits.  Binary16 holds 22 bits in two, with the row's largest element brought to 2^13 .. 2^14,
+// so that what is 2^-27 of it still has its bits and none overflows; bfloat16 24 bits in three, at any size.
 template <typename T> struct Parts;
 template <> struct Parts<_Float16> { static constexpr int N = 2; };
 template <> struct Parts<__bf16> { static constexpr int N = 3; };
 
-constexpr int kOutTile = 256;                    // elements of the outputs' rows that a workgroup takes
-
-// out[row][m] = y[row][m] + factor[row] * sum_k B[m][k] v[row][k] for 64 m of each wavefront, up to NS * 16 rows; 64 ranks at a time.
-template <typename T, typename Y, int NS>
-__device__ __forceinline__ void expand_tile(const T* B, int b_stride, int rank, float scale, int m0, int M, const Y* y, int64_t y_stride, Y* out,
-                                            int64_t out_stride, const int32_t* row, int rows, const float* v, int total, int64_t v_split, int splits,
-                                            x8<T>* vs, float* factor) {
-  constexpr int N = Parts<T>::N, MT = 4, PER = 16 / NS;    // threads a row
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, l16 = lane & 15, g = lane >> 4;
-  const int m_wave = m0 + 64 * wave;
-  f32x4 acc[MT][NS];
+// out[row][m] = y[row][m] + factor[row] * sum_k B[m][k] v[row][k] for the m of [m0, m1) and up to 64 rows, 32 * H ranks (H = 0: 16).  A wavefront
+// takes 16 rows, whose parts of v it holds in registers as operands, and 64 m at a time: four products side by side, whose results are 4
+// neighbouring m of 4 rows in every lane.  The next weights and elements of y are on their way meanwhile.  Where there are no more than 32 (16) rows,
+// two (four) wavefronts share the m.  Nothing passes through LDS, no wavefront waits for another.  Ranks that a bank does not have (three times 32
+// of four) read its last ones and meet zeros.
+template <typename T, typename Y, int H>
+__device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, const Tile& t, int rank, int m0, int m1) {
+  constexpr int N = Parts<T>::N, HV = H == 0 ? 1 : H;
+  constexpr int CH = H <= 2 ? HV : 2, CHUNKS = HV / CH, F = H == 0 ? 2 : 4 * CH;           // operands are taken CH * 32 ranks at a time
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
+  const int share = t.rows <= 16 ? 4 : t.rows <= 32 ? 2 : 1, stride = 64 * share;          // wavefronts that share 16 rows
+  const int sub = wave / share, first = m0 + 64 * (wave % share);
+  if (16 * sub >= t.rows || first >= m1) return;
+  const Bank bank(c.width, p.m, p.max_rank);
+  const x8<T>* B = slot_of<T>(c, p, t.slot) + bank.a_operands() * 64 + lane;
+  const bool has_y = p.y != nullptr;
+  int row[4];
+  const Y* y[4];
 #pragma unroll
-  for (int j = 0; j < MT; ++j)
+  for (int i = 0; i < 4; ++i) {
+    row[i] = __shfl(t.row, 16 * sub + 4 * g + i);
+    y[i] = has_y ? static_cast<const Y*>(p.y) + max(row[i], 0) * p.y_stride + 4 * l16 : reinterpret_cast<const Y*>(c.v);
+  }
+  auto load_w = [&](x8<T> (&w)[F], int m, int chunk) {
+    const int block = m / 64;
+    if (H == 0) {
 #pragma unroll
-    for (int s = 0; s < NS; ++s) acc[j][s] = f32x4{0.f, 0.f, 0.f, 0.f};
-  // thread: row tid / PER of the tile, ranks 4 * NS * (tid % PER) .. of a group
-  const int token = tid / PER, mine = 4 * NS * (tid % PER);
-  const bool there = token < rows;
-  const float* vr = v + (there ? (int64_t)row[token] * total : 0);
-  auto sums = [&](int k0, f32x4 (&x)[NS]) {
+      for (int f = 0; f < F; ++f) w[f] = B[(int64_t)(2 * block + f) * 64];
+    } else {
 #pragma unroll
-    for (int i = 0; i < NS; ++i) x[i] = f32x4{0.f, 0.f, 0.f, 0.f};
-    if (!there) return;
-#pragma unroll 4
+      for (int h = 0; h < CH; ++h)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) w[4 * h + j] = B[((int64_t)min(CH * chunk + h, bank.halves - 1) * bank.blocks + block) * 256 + 64 * j];
+    }
+  };
+  auto load_y = [&](Run4<Y> (&before)[4], int m) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) before[i] = *reinterpret_cast<const Run4<Y>*>(y[i] + (has_y ? m : 0));
+  };
+  // whole steps, then what is left
+  const int steps = (m1 - 64 - first + stride) / stride;                                   // (the first summands are above -stride: 0 at least)
+  x8<T> w[F], next_w[F];
+  Run4<Y> before[4], next_before[4];
+  load_w(w, first, 0);
+  if (steps > 0) load_y(before, first);
+  // the parts of v
+  x8<T> vs[N][H == 0 ? 2 : H];
+  float factor[4];
+  {
+    const int splits = c.cut.splits(t.count, c.rows), left = rank - 8 * (H == 0 ? g & 1 : g);
+    const float* v = v_of(c, 0, blockIdx.y, p.at, sub) + (H == 0 ? (g & 1) * 16 + l16 : lane) * 8;
+    const int64_t v_split = (int64_t)c.v_tiles * c.cut.rank_halves * (4 * 512);
+    const int halves = (p.max_rank + 31) / 32;
+    f32x4 x[HV][2];
+#pragma unroll
+    for (int h = 0; h < HV; ++h) x[h][0] = x[h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8 / HV
     for (int s = 0; s < splits; ++s)
 #pragma unroll
-      for (int i = 0; i < NS; ++i)
-        if (k0 + mine + 4 * i < rank) x[i] += *reinterpret_cast<const f32x4*>(vr + s * v_split + k0 + mine + 4 * i);
-#pragma unroll
-    for (int i = 0; i < NS; ++i)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        if (k0 + mine + 4 * i + e >= rank) x[i][e] = 0.f;
-  };
-  float up = 1.f;                                // what the row is multiplied with
-  if (N == 2) {
-    float top = 0.f;
-    for (int k0 = 0; k0 < rank; k0 += kGroup) {
-      f32x4 x[NS];
-      sums(k0, x);
-#pragma unroll
-      for (int i = 0; i < NS; ++i)
-#pragma unroll
-        for (int e = 0; e < 4; ++e) top = fmaxf(top, fabsf(x[i][e]));
-    }
-#pragma unroll
-    for (int d = 1; d < PER; d *= 2) top = fmaxf(top, __shfl_xor(top, d));
-    const int e = (int)(__float_as_uint(top) >> 23) - 127;                                 // of its leading bit
-    if (e < 128) up = __uint_as_float((uint32_t)(127 + 13 - max(e, -100)) << 23);
-  }
-  if (tid % PER == 0) factor[token] = scale / up;
-  for (int k0 = 0; k0 < rank; k0 += kGroup) {
-    x8<T> w[2][MT];
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int k = k0 + 32 * h + 8 * g;
-      const T* b = B + k;
-#pragma unroll
-      for (int j = 0; j < MT; ++j) {
-        w[h][j] = x8<T>{};
-        const int64_t m = min(m_wave + 16 * j + l16, M - 1);
-        if (k < rank) w[h][j] = operand_to(b + m * b_stride, 0, rank - k);
+      for (int h = 0; h < HV; ++h) {
+        const f32x4* from = reinterpret_cast<const f32x4*>(v + s * v_split + min(h, halves - 1) * (4 * 512));
+        x[h][0] += from[0];
+        x[h][1] += from[1];
       }
+    const bool live = 16 * sub + l16 < t.rows;
+    float top = 0.f, up = 1.f, mine = p.scale ? uniform(p.scale + t.slot) : 1.f;           // up: what the row is multiplied with
+#pragma unroll
+    for (int h = 0; h < HV; ++h)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        if (32 * h + e >= left || !live) x[h][e / 4][e % 4] = 0.f;
+        top = fmaxf(top, fabsf(x[h][e / 4][e % 4]));
+      }
+    if (N == 2) {
+      top = fmaxf(top, __shfl_xor(top, 16));
+      top = fmaxf(top, __shfl_xor(top, 32));
+      const int e = (int)(__float_as_uint(top) >> 23) - 127;                               // of its leading bit
+      if (e < 128) up = __uint_as_float((uint32_t)(127 + 13 - max(e, -100)) << 23);
+      mine /= up;
     }
-    f32x4 x[NS];
-    sums(k0, x);
-    if (k0 > 0) __syncthreads();                 // everyone is done with the last ranks
 #pragma unroll
-    for (int i = 0; i < NS; ++i) {
-      const int k = mine + 4 * i;
-      T* to = reinterpret_cast<T*>(vs + ((k >> 5) * NS + (token >> 4)) * 64 + (k >> 3 & 3) * 16 + (token & 15)) + (k & 7);
-      f32x4 rest = x[i] * up;
+    for (int i = 0; i < 4; ++i) factor[i] = __shfl(mine, 4 * g + i);
 #pragma unroll
-      for (int part = 0; part < N; ++part) {
-        Run4<T> piece;
+    for (int h = 0; h < HV; ++h)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          piece.e[e] = (T)rest[e];
-          rest[e] -= (float)piece.e[e];
+      for (int e = 0; e < 8; ++e) {
+        float rest = x[h][e / 4][e % 4] * up;
+#pragma unroll
+        for (int part = 0; part < N; ++part) {
+          const T piece = (T)rest;
+          rest -= (float)piece;
+          if (H == 0) {                          // for the operands' halves: ranks in the lower lanes, in the upper ones
+            vs[part][0][e] = g < 2 ? piece : (T)0.f;
+            vs[part][H == 0 ? 1 : 0][e] = g < 2 ? (T)0.f : piece;
+          } else {
+            vs[part][h][e] = piece;
+          }
         }
-        *reinterpret_cast<Run4<T>*>(to + part * 2 * NS * 64 * 8) = piece;
       }
-    }
-    __syncthreads();
+  }
+  auto multiply = [&](f32x4 (&acc)[4], const x8<T> (&w)[F], int chunk) {
+    if (H == 0) {
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
-      if (k0 + 32 * h < rank)
+      for (int part = 0; part < N; ++part)
+#pragma unroll
+        for (int j = 0; j < 4; ++j) acc[j] = mfma(vs[part][H == 0 ? j & 1 : 0], w[(j >> 1) % F], acc[j]);
+    } else {
+#pragma unroll
+      for (int h = 0; h < CH; ++h)
 #pragma unroll
         for (int part = 0; part < N; ++part)
 #pragma unroll
-          for (int s = 0; s < NS; ++s) {
-            const x8<T> b = vs[((part * 2 + h) * NS + s) * 64 + lane];
+          for (int j = 0; j < 4; ++j) acc[j] = mfma(vs[part][(CH * chunk + h) % HV], w[(4 * h + j) % F], acc[j]);
+    }
+  };
+  auto zero = [](f32x4 (&acc)[4]) {
 #pragma unroll
-            for (int j = 0; j < MT; ++j) acc[j][s] = mfma(w[h][j], b, acc[j][s]);
-          }
-  }
+    for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
+  };
+  auto store = [&](const f32x4 (&acc)[4], const Run4<Y> (&before)[4], int m) {
 #pragma unroll
-  for (int s = 0; s < NS; ++s) {
-    const int token = 16 * s + l16;
-    if (token >= rows) continue;
-    const int64_t t = row[token];
-    const float f = factor[token];
+    for (int i = 0; i < 4; ++i) {
+      Run4<Y> o;
 #pragma unroll
-    for (int j = 0; j < MT; ++j) {
-      const int m = m_wave + 16 * j + 4 * g;
-      if (m + 4 <= M) {
-        Run4<Y> o;
-        if (y) o = *reinterpret_cast<const Run4<Y>*>(y + t * y_stride + m);
+      for (int j = 0; j < 4; ++j) o.e[j] = (Y)fmaf(factor[i], acc[j][i], has_y ? (float)before[i].e[j] : 0.f);
+      if (row[i] >= 0) *reinterpret_cast<Run4<Y>*>(static_cast<Y*>(p.out) + row[i] * p.out_stride + m + 4 * l16) = o;
+    }
+  };
+  auto step = [&](x8<T> (&w)[F], x8<T> (&next_w)[F], const Run4<Y> (&before)[4], Run4<Y> (&next_before)[4], int m, int next) {
+    f32x4 acc[4];
+    zero(acc);
+    load_y(next_before, next);
+    if (CHUNKS == 1) {
+      load_w(next_w, next, 0);
+      multiply(acc, w, 0);
+    } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) o.e[e] = (Y)fmaf(f, acc[j][s][e], y ? (float)o.e[e] : 0.f);
-        *reinterpret_cast<Run4<Y>*>(out + t * out_stride + m) = o;
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (m + e < M) out[t * out_stride + m + e] = (Y)fmaf(f, acc[j][s][e], y ? (float)y[t * y_stride + m + e] : 0.f);
+      for (int k = 0; k < CHUNKS; k += 2) {      // w: this chunk, next_w: the one after it
+        load_w(next_w, m, k + 1);
+        multiply(acc, w, k);
+        load_w(w, k + 2 < CHUNKS ? m : next, k + 2 < CHUNKS ? k + 2 : 0);
+        multiply(acc, next_w, k + 1);
       }
     }
+    store(acc, before, m);
+  };
+  int m = first;
+  const int end = first + stride * steps, behind = end - stride;                           // (behind the last step it is loaded again)
+  for (; m < end; m += 2 * stride) {
+    step(w, next_w, before, next_before, m, min(m + stride, behind));
+    if (m + stride >= end) break;
+    if (CHUNKS == 1) step(next_w, w, next_before, before, m + stride, min(m + 2 * stride, behind));
+    else step(w, next_w, next_before, before, m + stride, min(m + 2 * stride, behind));
   }
-}
-
-// Rows that no adapter changes.
-template <typename Y>
-__device__ __forceinline__ void copy_tile(int m0, int M, const Y* y, int64_t y_stride, Y* out, int64_t out_stride, const int32_t* row, int rows) {
-  if (y == out && y_stride == out_stride) return;
-  const int m = m0 + threadIdx.x;
-  if (m >= M) return;
-  for (int i = 0; i < rows; ++i) out[row[i] * out_stride + m] = y ? y[row[i] * y_stride + m] : (Y)0.f;
-}
-
-template <typename T, typename Y>
-__global__ void __launch_bounds__(256) expand_kernel(spqr_adapters_t a, spqr_adapter_plan_t plan, Cut cut, const float* v, int out_tiles) {
-  __shared__ x8<T> vs[Parts<T>::N * 2 * 4 * 64];
-  __shared__ float factor[kTile];
-  __shared__ int32_t row[kTile];
-  const int tiles = min(plan.count[0], plan.max_tiles), splits = cut.splits(tiles, plan.rows);
-  for (int64_t i = blockIdx.x; i < (int64_t)tiles * out_tiles; i += gridDim.x) {
-    const int t = (int)(i / out_tiles);
-    int rows, p = 0, c = (int)(i % out_tiles), at = 0;
-    const int slot = tile_of(plan, a, t, &rows);
-    for (; c >= (a.m[p] + kOutTile - 1) / kOutTile; ++p) { c -= (a.m[p] + kOutTile - 1) / kOutTile; at += padded(a.max_rank[p]); }
-    const int rank = slot < 0 ? 0 : rank_of(a, p, slot), M = a.m[p];
-    __syncthreads();                             // everyone is done with the last tile
-    rows = rows_of_tile(plan, t, rows, row);
-    const Y* y = static_cast<const Y*>(a.y[p]);
-    Y* out = static_cast<Y*>(a.out[p]);
-    if (rank <= 0) {
-      copy_tile(kOutTile * c, M, y, a.y_stride[p], out, a.out_stride[p], row, rows);
-      continue;
+  if (end < m1) {
+    f32x4 acc[4];
+    zero(acc);
+#pragma unroll
+    for (int k = 0; k < CHUNKS; ++k) {
+      load_w(w, end, k);
+      multiply(acc, w, k);
     }
-    const T* B = static_cast<const T*>(a.B[p]) + (int64_t)slot * M * a.max_rank[p];
-    const float scale = a.scale[p] ? a.scale[p][slot] : 1.f;
-    const int64_t v_split = (int64_t)plan.rows * cut.total;
-#define SPQR_EXPAND(NS) expand_tile<T, Y, NS>(B, a.max_rank[p], rank, scale, kOutTile * c, M, y, a.y_stride[p], out, a.out_stride[p], row, rows, v + at, cut.total, v_split, splits, vs, factor)
-    if (rows <= 16) SPQR_EXPAND(1);
-    else if (rows <= 32) SPQR_EXPAND(2);
-    else SPQR_EXPAND(4);
-#undef SPQR_EXPAND
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int at = end + 4 * l16 + j;
+        if (at < m1 && row[i] >= 0)
+          static_cast<Y*>(p.out)[row[i] * p.out_stride + at] = (Y)fmaf(factor[i], acc[j][i], has_y ? (float)y[i][end + j] : 0.f);
+      }
   }
+}
+
+// Rows that no adapter changes: a wavefront takes 256 elements of a row, four such pieces on their way at once.
+template <typename Y>
+__device__ __forceinline__ void copy_rows(const Projection& p, const Tile& t, int m0, int m1) {
+  const Y* y = static_cast<const Y*>(p.y);
+  Y* out = static_cast<Y*>(p.out);
+  if (y == out && p.y_stride == p.out_stride) return;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = t.rows * ((m1 - m0 + 255) / 256);
+  for (int i0 = wave; i0 < pieces; i0 += 16) {
+    Run4<Y> x[4];
+    int64_t row[4];
+    int m[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int piece = min(i0 + 4 * i, pieces - 1);
+      row[i] = __shfl(t.row, piece % t.rows);
+      m[i] = m0 + 256 * (piece / t.rows) + 4 * lane;
+      if (i0 + 4 * i >= pieces) row[i] = -1;
+      const int64_t at = max(row[i], (int64_t)0) * p.y_stride;
+      if (!y) x[i] = Run4<Y>{};
+      else if (m0 + 256 * (piece / t.rows) + 256 <= m1) x[i] = *reinterpret_cast<const Run4<Y>*>(y + at + m[i]);
+      else
+#pragma unroll
+        for (int e = 0; e < 4; ++e) x[i].e[e] = y[at + min(m[i] + e, m1 - 1)];
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (row[i] >= 0) {
+        Y* to = out + row[i] * p.out_stride + m[i];
+        if (m[i] + 4 <= m1) *reinterpret_cast<Run4<Y>*>(to) = x[i];
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (m[i] + e < m1) to[e] = x[i].e[e];
+      }
+  }
+}
+
+// LONG: ranks above 64.
+template <typename T, typename Y, bool LONG>
+__global__ void __launch_bounds__(256) expand_kernel(Call c) {
+  const Projection& p = c.p[blockIdx.z];
+  const int m0 = c.span * (int)blockIdx.x, m1 = min(p.m, m0 + c.span);
+  if (m0 >= m1) return;
+  const Tile t = tile_at(c, blockIdx.y);
+  if (t.rows == 0) return;
+  const int rank = rank_of(p, t.slot);
+  if (rank <= 0) copy_rows<Y>(p, t, m0, m1);
+  else if (p.max_rank <= 16) expand_rows<T, Y, 0>(c, p, t, rank, m0, m1);
+  else if (rank <= 32) expand_rows<T, Y, 1>(c, p, t, rank, m0, m1);
+  else if (!LONG || rank <= 64) expand_rows<T, Y, 2>(c, p, t, rank, m0, m1);
+  else if (rank <= 128) expand_rows<T, Y, LONG ? 4 : 2>(c, p, t, rank, m0, m1);
+  else expand_rows<T, Y, LONG ? 8 : 2>(c, p, t, rank, m0, m1);
 }
 
 static int check_bank(const spqr_adapters_t* a) {
   if (!a) return SPQR_ERR_NULL;
   if (a->count < 1 || a->count > SPQR_MAX_FUSED) return SPQR_ERR_PARAM;
-  if (a->width < 1 || a->width > SPQR_MAX_WIDTH) return SPQR_ERR_SHAPE;
-  for (int p = 0; p < a->count; ++p)
+  if (a->width < 1 || a->width > SPQR_MAX_WIDTH || a->slots < 1 || a->slots > SPQR_MAX_SLOTS) return SPQR_ERR_SHAPE;
+  for (int p = 0; p < a->count; ++p) {
     if (a->max_rank[p] < 1 || a->max_rank[p] > SPQR_MAX_RANK) return SPQR_ERR_PARAM;
+    if (a->m[p] < 1 || a->m[p] > SPQR_MAX_WIDTH) return SPQR_ERR_SHAPE;
+  }
   return SPQR_OK;
 }
 
 static Cut cut_of(const spqr_adapters_t* a) {
-  Cut c{0, (a->width + kUnit - 1) / kUnit, 0};
+  Cut c{0, 0, (a->width + kStage - 1) / kStage};
   for (int p = 0; p < a->count; ++p) {
-    c.groups += (a->max_rank[p] + kGroup - 1) / kGroup;
-    c.total += padded(a->max_rank[p]);
+    c.rank_tiles += (a->max_rank[p] + 15) / 16;
+    c.rank_halves += (a->max_rank[p] + 31) / 32;
+  }
+  return c;
+}
+
+static Call call_of(const spqr_adapters_t* a, const spqr_adapter_plan_t* plan, int tiles) {
+  Call c;
+  c.cut = cut_of(a);
+  c.x = a->x; c.x_stride = a->x_stride; c.width = a->width; c.slots = a->slots;
+  c.count = plan->count; c.tile = plan->tile; c.row = plan->row; c.rows = plan->rows; c.max_tiles = c.v_tiles = tiles;
+  c.v = static_cast<float*>(a->workspace);
+  int at = 0, tile = 0;
+  for (int p = 0; p < SPQR_MAX_FUSED; ++p) {
+    if (p >= a->count) { c.p[p] = Projection{}; continue; }
+    c.p[p] = Projection{static_cast<const uint8_t*>(a->bank[p]), a->scale[p], a->y[p], a->out[p], a->y_stride[p], a->out_stride[p], a->m[p], a->max_rank[p], at};
+    at += (a->max_rank[p] + 31) / 32;
+    for (int k = 0; k < a->max_rank[p]; k += 16) c.rank_tile[tile++] = p + 256 * (k / 16);
   }
   return c;
 }
 
 template <typename T, typename Y>
-static int launch_adapters(const spqr_adapters_t& a, const spqr_adapter_plan_t& plan, int tiles, hipStream_t st) {
-  float* v = static_cast<float*>(a.workspace);
-  const Cut cut = cut_of(&a);
-  int out_tiles = 0;
-  for (int p = 0; p < a.count; ++p) out_tiles += (a.m[p] + kOutTile - 1) / kOutTile;
-  // As many workgroups as the most tiles there can be give work; those that are too many end at once.
-  const int64_t shrink = (int64_t)tiles * cut.groups, expand = (int64_t)tiles * out_tiles;
-  const int shrink_grid = (int)(shrink < kShrinkGroups ? shrink * kMostSplits < kShrinkGroups ? shrink * kMostSplits : kShrinkGroups : shrink < 65536 ? shrink : 65536);
-  hipLaunchKernelGGL((shrink_kernel<T>), dim3(shrink_grid), dim3(256), 0, st, a, plan, cut, v);
-  hipLaunchKernelGGL((expand_kernel<T, Y>), dim3((unsigned)(expand < 65536 ? expand : 65536)), dim3(256), 0, st, a, plan, cut, v, out_tiles);
-  return launched();
+static void launch_expand(const Call& c, bool longer, dim3 grid, hipStream_t st) {
+  if (longer) hipLaunchKernelGGL((expand_kernel<T, Y, true>), grid, dim3(256), 0, st, c);
+  else hipLaunchKernelGGL((expand_kernel<T, Y, false>), grid, dim3(256), 0, st, c);
 }
 
 template <typename T>
-static int launch_for(const spqr_adapters_t& a, const spqr_adapter_plan_t& plan, int tiles, hipStream_t st) {
-  if (a.y_dtype == SPQR_F32) return launch_adapters<T, float>(a, plan, tiles, st);
-  if (a.y_dtype == SPQR_F16) return launch_adapters<T, _Float16>(a, plan, tiles, st);
-  return launch_adapters<T, __bf16>(a, plan, tiles, st);
+static int launch_adapters(Call& c, int count, int y_dtype, int tiles, hipStream_t st) {
+  int most = 0, groups = 0;
+  int64_t all = 0;
+  bool longer = false;
+  for (int p = 0; p < count; ++p) {
+    most = c.p[p].m > most ? c.p[p].m : most;
+    all += (c.p[p].m + 255) / 256;
+    groups += (c.p[p].max_rank + 16 * kWaveTiles - 1) / (16 * kWaveTiles);
+    longer = longer || c.p[p].max_rank > 64;
+  }
+  const int64_t rounds = all * tiles / kExpandGroups;
+  c.span = 256 * (int)(rounds < 1 ? 1 : rounds < kMostRounds ? rounds : kMostRounds);
+  // Workgroups for the most tiles and parts that there can be, and for the widest output; those that are too many end at once.
+  const dim3 shrink(c.cut.splits(1, c.rows), tiles, groups), expand((most + c.span - 1) / c.span, tiles, count);
+  hipLaunchKernelGGL((shrink_kernel<T>), shrink, dim3(256), 0, st, c);
+  if (y_dtype == SPQR_F32) launch_expand<T, float>(c, longer, expand, st);
+  else if (y_dtype == SPQR_F16) launch_expand<T, _Float16>(c, longer, expand, st);
+  else launch_expand<T, __bf16>(c, longer, expand, st);
+  return launched();
 }
 
 }  // namespace spqr_blk
@@ -469,18 +710,41 @@ extern "C" int spqr_adapter_plan(const spqr_adapter_plan_t* p, void* stream) {
   return launched();
 }
 
+extern "C" int64_t spqr_adapters_bank_bytes(const spqr_adapters_t* a, int32_t p) {
+  const int rc = check_bank(a);
+  if (rc) return rc;
+  if (p < 0 || p >= a->count) return SPQR_ERR_PARAM;
+  return header_bytes(a->slots) + a->slots * Bank(a->width, a->m[p], a->max_rank[p]).operands() * 1024;
+}
+
+extern "C" int spqr_adapters_pack(const spqr_adapters_t* a, int32_t p, int32_t first, int32_t slots, const void* A, const void* B, const int32_t* rank,
+                                  void* stream) {
+  const int rc = check_bank(a);
+  if (rc) return rc;
+  if (p < 0 || p >= a->count || first < 0 || slots < 0 || first > a->slots - slots) return SPQR_ERR_PARAM;
+  if (a->dtype != SPQR_F16 && a->dtype != SPQR_BF16) return SPQR_ERR_DTYPE;
+  if (slots == 0) return SPQR_OK;
+  if (!A || !B || !a->bank[p]) return SPQR_ERR_NULL;
+  if (!aligned(A, 2) || !aligned(B, 2) || !aligned(rank, 4) || !aligned(a->bank[p], 256)) return SPQR_ERR_ALIGN;
+  const Pack args{static_cast<const uint16_t*>(A), static_cast<const uint16_t*>(B), rank, static_cast<uint8_t*>(const_cast<void*>(a->bank[p])), a->width, a->m[p],
+                  a->max_rank[p], a->slots, first};
+  const int64_t groups = (Bank(a->width, a->m[p], a->max_rank[p]).operands() * 64 + 255) / 256;
+  hipLaunchKernelGGL(pack_kernel, dim3((unsigned)(groups < 1024 ? groups : 1024), slots), dim3(256), 0, static_cast<hipStream_t>(stream), args);
+  return launched();
+}
+
 extern "C" int64_t spqr_adapters_workspace_bytes(const spqr_adapters_t* a, int32_t rows) {
   const int rc = check_bank(a);
   if (rc) return rc;
   if (rows < 0 || rows > SPQR_MAX_ROWS) return SPQR_ERR_SHAPE;
-  // as many parts of the sums as steps of up to so many rows are cut into
+  // as many parts of the sums, for as many tiles, as a step of up to so many rows can have
   const Cut cut = cut_of(a);
   int64_t most = 0;
-  for (int64_t n = rows; n > 0; n = (n + kTile - 1) / kTile - 1 > 0 ? ((n + kTile - 1) / kTile - 1) * kTile : 0) {
-    const int64_t floats = n * cut.splits(1, (int)n);
-    most = floats > most ? floats : most;
+  for (int64_t n = rows; n > 0; n = ((n + kTile - 1) / kTile - 1) * kTile) {
+    const int64_t parts = (int64_t)spqr_adapter_tiles((int32_t)n, a->slots) * cut.splits(1, (int)n);
+    most = parts > most ? parts : most;
   }
-  return (most * cut.total * 4 + 255) / 256 * 256;
+  return most * cut.rank_halves * (4 * 512 * 4);
 }
 
 extern "C" int spqr_adapters(const spqr_adapters_t* a, const spqr_adapter_plan_t* plan, void* stream) {
@@ -493,20 +757,18 @@ extern "C" int spqr_adapters(const spqr_adapters_t* a, const spqr_adapter_plan_t
   const int64_t most = INT64_MAX / 8 / (rows > 0 ? rows : 1);
   if (a->x_stride < a->width || a->x_stride > most) return SPQR_ERR_SHAPE;
   for (int p = 0; p < a->count; ++p)
-    if (a->m[p] < 1 || a->m[p] > SPQR_MAX_WIDTH || (a->y[p] && (a->y_stride[p] < a->m[p] || a->y_stride[p] > most)) || a->out_stride[p] < a->m[p] ||
-        a->out_stride[p] > most)
-      return SPQR_ERR_SHAPE;
+    if ((a->y[p] && (a->y_stride[p] < a->m[p] || a->y_stride[p] > most)) || a->out_stride[p] < a->m[p] || a->out_stride[p] > most) return SPQR_ERR_SHAPE;
   if (rows == 0) return SPQR_OK;
   if (!a->x || !a->workspace) return SPQR_ERR_NULL;
   if (!aligned(a->x, 2) || !aligned(a->workspace, 256)) return SPQR_ERR_ALIGN;
   for (int p = 0; p < a->count; ++p) {
-    if (!a->A[p] || !a->B[p] || !a->out[p]) return SPQR_ERR_NULL;
-    if (!aligned(a->A[p], 2) || !aligned(a->B[p], 2) || !aligned(a->rank[p], 4) || !aligned(a->scale[p], 4) ||
-        !aligned(a->y[p], size_of(a->y_dtype)) || !aligned(a->out[p], size_of(a->y_dtype)))
+    if (!a->bank[p] || !a->out[p]) return SPQR_ERR_NULL;
+    if (!aligned(a->bank[p], 256) || !aligned(a->scale[p], 4) || !aligned(a->y[p], size_of(a->y_dtype)) || !aligned(a->out[p], size_of(a->y_dtype)))
       return SPQR_ERR_ALIGN;
   }
   if (a->workspace_bytes < spqr_adapters_workspace_bytes(a, rows)) return SPQR_ERR_WORKSPACE;
   const int tiles = spqr_adapter_tiles(rows, plan->slots);
   const hipStream_t st = static_cast<hipStream_t>(stream);
-  return a->dtype == SPQR_F16 ? launch_for<_Float16>(*a, *plan, tiles, st) : launch_for<__bf16>(*a, *plan, tiles, st);
+  Call c = call_of(a, plan, tiles);
+  return a->dtype == SPQR_F16 ? launch_adapters<_Float16>(c, a->count, a->y_dtype, tiles, st) : launch_adapters<__bf16>(c, a->count, a->y_dtype, tiles, st);
 }

@@ -99,12 +99,14 @@ def bank(width, ms, ranks, slots, dtype="f16", seed=0, mixed=True, per_projectio
                 k = int((rank[p] if per_projection else rank)[s])
                 A[p][s, k:] = math.nan if s % 2 else math.inf
                 B[p][s, :, k:] = math.nan
-    return K.SpQRAdapters(A, B, rank=rank, scale=scale, rows=rows)
+    b = K.SpQRAdapters(A, B, rank=rank, scale=scale, rows=rows)
+    b.plain = A, B, rank if isinstance(rank, list) else [rank] * len(ms), [scale] * len(ms)
+    return b
 
 
 def reference(b, adapter_of_row, x, ys):
     """Of each projection: the result, and a bound of its error before the last rounding."""
-    A, B, rank, scale = b._kept
+    A, B, rank, scale = b.plain
     found = []
     for p in range(len(A)):
         out = ys[p].double().clone() if ys is not None else torch.zeros(x.shape[0], B[p].shape[1], dtype=torch.float64, device="cuda")
@@ -280,6 +282,28 @@ def test_beside_the_shared_projection_out_of_a_graph_on_another_stream():
         torch.cuda.synchronize()
         for a, c in zip(ys, want):
             assert (a - c).abs().max() <= 1e-5 * c.abs().max()   # a captured fused product may add its parts in another order
+
+
+def test_slots_are_refilled():
+    """Other adapters in some slots: their rows change, the others' do not."""
+    b, plan, x, ys, got = run(300, [100, 64], [24, 24], 5, [0, 1, 2, 3, 4, -1, 2], mixed=False)
+    other = bank(300, [100, 64], [24, 24], 2, seed=9, mixed=False)
+    A, B, _, _ = other.plain
+    rank = ints([24, 5])
+    for p in range(2):
+        A[p][1, 5:], B[p][1, :, 5:] = math.nan, math.inf
+    b.load(2, A, B, rank)
+    for p in range(2):
+        b.plain[0][p][2:4], b.plain[1][p][2:4] = A[p], B[p]
+    b.plain[2][:] = [ints([24, 24, 24, 5, 24])] * 2
+    again = K.spqr_adapters(b, plan, x, ys)
+    for p, (out, bound) in enumerate(reference(b, [0, 1, 2, 3, 4, -1, 2], x, ys)):
+        close(again[p], out, bound)
+        assert torch.equal(again[p][[0, 1, 4, 5]], got[p][[0, 1, 4, 5]]) and not torch.equal(again[p][[2, 3, 6]], got[p][[2, 3, 6]])
+    for first, count in ((-1, 2), (4, 2)):
+        with pytest.raises(ValueError):
+            b.load(first, A, B)
+    b.load(5, [a[:0] for a in A], [v[:0] for v in B])
 
 
 def test_refusals_of_the_binding():

@@ -43,7 +43,7 @@ def plan(**change):
 
 
 def bank(**change):
-    at = {n: [SOME + 4096 * (2 * i + p) for p in range(2)] for i, n in enumerate(("A", "B", "rank", "scale", "y", "out"))}
+    at = {n: [SOME + 4096 * (2 * i + p) for p in range(2)] for i, n in enumerate(("bank", "scale", "y", "out"))}
     return filled(K.spqr_adapters_t(), dict(count=2, width=64, slots=5, dtype=F16, y_dtype=F32, m=[96, 32], max_rank=[16, 8], y_stride=[96, 32],
                                             out_stride=[96, 32], x=SOME, x_stride=64, workspace=SOME, workspace_bytes=1 << 40, **at), change)
 
@@ -66,7 +66,7 @@ def test_every_declared_symbol_is_exported_and_the_descriptors_have_the_headers_
     text = open(os.path.join(ROOT, "include", "spqr_block.h")).read()
     text = re.sub(r"/\*.*?\*/", "", text, flags=re.S)
     names = set(re.findall(r"\b(spqr_[a-z_0-9]+)\s*\(", text))
-    assert names == {"spqr_residual_norm", "spqr_adapter_tiles", "spqr_adapter_plan", "spqr_adapters_workspace_bytes", "spqr_adapters",
+    assert names == {"spqr_residual_norm", "spqr_adapter_tiles", "spqr_adapter_plan", "spqr_adapters_bank_bytes", "spqr_adapters_pack", "spqr_adapters_workspace_bytes", "spqr_adapters",
                      "spqr_token_logprobs_workspace_bytes", "spqr_token_logprobs"}
     for n in names:
         assert hasattr(C.CDLL(P.library_path()), n)
@@ -127,12 +127,32 @@ def test_tiles_are_enough_for_any_rows():
 @pytest.mark.parametrize("field,value,status", [
     ("count", 0, PARAM), ("count", 9, PARAM), ("width", 0, SHAPE), ("width", 65537, SHAPE), ("slots", 4, PARAM), ("dtype", F32, DTYPE), ("dtype", 3, DTYPE),
     ("y_dtype", 3, DTYPE), ("m", [96, 0], SHAPE), ("m", [65537], SHAPE), ("max_rank", [16, 0], PARAM), ("max_rank", [257], PARAM), ("x_stride", 63, SHAPE),
-    ("y_stride", [96, 31], SHAPE), ("out_stride", [95], SHAPE), ("out_stride", [1 << 62], SHAPE), ("A", [None], NULL), ("B", [SOME, None], NULL),
-    ("out", [None], NULL), ("x", None, NULL), ("workspace", None, NULL), ("x", SOME + 1, ALIGN), ("A", [SOME + 1], ALIGN), ("B", [SOME, SOME + 1], ALIGN),
-    ("rank", [SOME + 2], ALIGN), ("scale", [SOME + 2], ALIGN), ("y", [SOME + 2], ALIGN), ("out", [SOME, SOME + 2], ALIGN), ("workspace", SOME + 128, ALIGN),
+    ("y_stride", [96, 31], SHAPE), ("out_stride", [95], SHAPE), ("out_stride", [1 << 62], SHAPE), ("bank", [None], NULL), ("bank", [SOME, None], NULL),
+    ("out", [None], NULL), ("x", None, NULL), ("workspace", None, NULL), ("x", SOME + 1, ALIGN), ("bank", [SOME + 128], ALIGN), ("scale", [SOME + 2], ALIGN), ("y", [SOME + 2], ALIGN), ("out", [SOME, SOME + 2], ALIGN), ("workspace", SOME + 128, ALIGN),
     ("workspace_bytes", 0, WORKSPACE), ("workspace_bytes", -1, WORKSPACE)])
 def test_adapters_refuse(field, value, status):
     assert adapt(**{field: value}) == status
+
+
+def pack(p=0, first=0, slots=5, A=SOME, B=SOME, rank=SOME, **change):
+    return K._lib().spqr_adapters_pack(C.byref(bank(**change)), p, first, slots, A, B, rank, None)
+
+
+def test_pack_refuses():
+    assert pack(p=-1) == PARAM and pack(p=2) == PARAM and pack(first=-1) == PARAM and pack(first=1) == PARAM and pack(slots=-1) == PARAM and pack(slots=6) == PARAM
+    assert pack(first=5, slots=0, A=None) == OK and pack(dtype=F32) == DTYPE and pack(max_rank=[0]) == PARAM and pack(width=0) == SHAPE
+    assert pack(A=None) == NULL and pack(B=None) == NULL and pack(bank=[None]) == NULL
+    assert pack(A=SOME + 1) == ALIGN and pack(B=SOME + 1) == ALIGN and pack(rank=SOME + 2) == ALIGN and pack(bank=[SOME + 128]) == ALIGN
+
+
+def test_bank_bytes():
+    """Ranks rounded up to 16 (A) and 32 (B, above 16), widths to 128, m to 64."""
+    lib = K._lib()
+    for width, m, rank, elements in ((64, 96, 16, 16 * 128 + 128 * 16), (129, 64, 17, 32 * 256 + 64 * 32), (1, 1, 1, 16 * 128 + 64 * 16),
+                                     (8192, 8192, 64, 2 * 64 * 8192), (128, 64, 40, 48 * 128 + 64 * 64)):
+        assert lib.spqr_adapters_bank_bytes(C.byref(bank(width=width, m=[m, 32], max_rank=[rank, 8])), 0) == 256 + 5 * 2 * elements
+    assert lib.spqr_adapters_bank_bytes(C.byref(bank()), 2) == PARAM and lib.spqr_adapters_bank_bytes(None, 0) == NULL
+    assert lib.spqr_adapters_bank_bytes(C.byref(bank(slots=4097)), 0) == SHAPE
 
 
 def test_adapters_refuse_a_plan_that_is_none():
@@ -142,7 +162,7 @@ def test_adapters_refuse_a_plan_that_is_none():
 
 def test_the_adapters_workspace_goes_by_the_sizes():
     lib = K._lib()
-    got = [lib.spqr_adapters_workspace_bytes(C.byref(bank(x=None, workspace=None, A=[None] * 2)), n) for n in (0, 1, 16, 200, 5000)]
+    got = [lib.spqr_adapters_workspace_bytes(C.byref(bank(x=None, workspace=None, bank=[None] * 2)), n) for n in (0, 1, 16, 200, 5000)]
     assert all(b % 256 == 0 for b in got) and got[0] == 0 and 0 < got[1] and got == sorted(got)
     assert adapt(workspace_bytes=lib.spqr_adapters_workspace_bytes(C.byref(bank()), 130) - 1) == WORKSPACE
     assert lib.spqr_adapters_workspace_bytes(C.byref(bank()), -1) == SHAPE and lib.spqr_adapters_workspace_bytes(C.byref(bank()), (1 << 20) + 1) == SHAPE
