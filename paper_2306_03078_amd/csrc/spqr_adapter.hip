@@ -175,7 +175,6 @@ __global__ void __launch_bounds__(256) pack_kernel(Pack a) {
 constexpr int kStage = 128;                      // elements of x at a time
 constexpr int kMostSplits = 8;
 constexpr int kShrinkGroups = 512;               // workgroups that A x is split into where tiles are few
-constexpr int kExpandGroups = 768, kMostRounds = 4;
 constexpr int kWaveTiles = 4;                    // tiles of 16 ranks that a wavefront takes at once
 
 // How a call is cut: into how many parts the sum over the elements of x, for the tiles that there are (no fewer than the step's rows may
@@ -211,7 +210,7 @@ struct Call {
   float* v;                                      // A x: [splits][tiles][blocks of 32 ranks][16 rows: 4][lane][8], as the operands of the next product
   Cut cut;
   int width, slots, rows, max_tiles, v_tiles;
-  int span;                                      // elements of the outputs' rows that a workgroup takes
+  int pieces;                                    // of 256 elements, of a row of all outputs
   int rank_tile[SPQR_MAX_FUSED * SPQR_MAX_RANK / 16];      // projection + 256 * its tile of 16 ranks
 };
 __device__ __forceinline__ float* v_of(const Call& c, int split, int tile, int half, int sub) {
@@ -387,29 +386,28 @@ template <typename T> struct Parts;
 template <> struct Parts<_Float16> { static constexpr int N = 2; };
 template <> struct Parts<__bf16> { static constexpr int N = 3; };
 
-// out[row][m] = y[row][m] + factor[row] * sum_k B[m][k] v[row][k] for the m of [m0, m1) and up to 64 rows, 32 * H ranks (H = 0: 16).  A wavefront
-// takes 16 rows, whose parts of v it holds in registers as operands, and 64 m at a time: four products side by side, whose results are 4
-// neighbouring m of 4 rows in every lane.  The next weights and elements of y are on their way meanwhile.  Where there are no more than 32 (16) rows,
-// two (four) wavefronts share the m.  Nothing passes through LDS, no wavefront waits for another.  Ranks that a bank does not have (three times 32
-// of four) read its last ones and meet zeros.
-template <typename T, typename Y, int H>
-__device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, const Tile& t, int rank, int m0, int m1) {
-  constexpr int N = Parts<T>::N, HV = H == 0 ? 1 : H;
-  constexpr int CH = H <= 2 ? HV : 2, CHUNKS = HV / CH, F = H == 0 ? 2 : 4 * CH;           // operands are taken CH * 32 ranks at a time
+// out[row][m] = y[row][m] + factor[row] * sum_k B[m][k] v[row][k] for the m of [m0, m1) and up to 64 rows, 32 * H ranks (H = 0: 16).  The parts of v
+// lie in LDS as operands, NS * 16 rows of them.  A wavefront takes 64 m at a time, four products side by side, whose results are 4 neighbouring m
+// of 4 rows in every lane; the workgroup's four are neighbours, so that a row is read and written 1 KB at a time (wavefronts with rows of their
+// own and 256 bytes of each: 144 us in place of XX for the rows of adapt-prompts).  The next weights and elements of y are on their way meanwhile.
+// Ranks that a bank does not have (three times 32 of four) read its last ones and meet zeros.
+template <typename T, typename Y, int H, int NS>
+__device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, const Tile& t, int tile, int sub0, int rank, int m0, int m1, f32x4* sums,
+                                            x8<T>* vs, float* factors) {
+  constexpr int N = Parts<T>::N, HV = H == 0 ? 1 : H, HL = H == 0 ? 2 : H;                 // operands of a row's ranks
+  constexpr int CH = H <= 2 ? HV : 2, CHUNKS = HV / CH, F = H == 0 ? 2 : 4 * CH;           // weights are taken CH * 32 ranks at a time
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), l16 = lane & 15, g = lane >> 4;
-  const int share = t.rows <= 16 ? 4 : t.rows <= 32 ? 2 : 1, stride = 64 * share;          // wavefronts that share 16 rows
-  const int sub = wave / share, first = m0 + 64 * (wave % share);
-  if (16 * sub >= t.rows || first >= m1) return;
   const Bank bank(c.width, p.m, p.max_rank);
   const x8<T>* B = slot_of<T>(c, p, t.slot) + bank.a_operands() * 64 + lane;
   const bool has_y = p.y != nullptr;
-  int row[4];
-  const Y* y[4];
+  const Y* const y = has_y ? static_cast<const Y*>(p.y) + 4 * l16 : reinterpret_cast<const Y*>(c.v);
+  Y* const out = static_cast<Y*>(p.out) + 4 * l16;
+  const int64_t y_stride = has_y ? p.y_stride : 0, out_stride = p.out_stride;
+  int row[NS][4];
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    row[i] = __shfl(t.row, 16 * sub + 4 * g + i);
-    y[i] = has_y ? static_cast<const Y*>(p.y) + max(row[i], 0) * p.y_stride + 4 * l16 : reinterpret_cast<const Y*>(c.v);
-  }
+  for (int s = 0; s < NS; ++s)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) row[s][i] = __shfl(t.row, 16 * (sub0 + s) + 4 * g + i);
   auto load_w = [&](x8<T> (&w)[F], int m, int chunk) {
     const int block = m / 64;
     if (H == 0) {
@@ -422,37 +420,68 @@ __device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, 
         for (int j = 0; j < 4; ++j) w[4 * h + j] = B[((int64_t)min(CH * chunk + h, bank.halves - 1) * bank.blocks + block) * 256 + 64 * j];
     }
   };
-  auto load_y = [&](Run4<Y> (&before)[4], int m) {
-#pragma unroll
-    for (int i = 0; i < 4; ++i) before[i] = *reinterpret_cast<const Run4<Y>*>(y[i] + (has_y ? m : 0));
+  // (A row's address is worked out where it is needed: kept for all rows they would take half of the registers.)
+  auto fresh = [](int row) {
+    asm volatile("" : "+v"(row));
+    return row;
   };
-  // whole steps, then what is left
-  const int steps = (m1 - 64 - first + stride) / stride;                                   // (the first summands are above -stride: 0 at least)
+  auto load_y = [&](Run4<Y> (&before)[4], int s, int m) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) before[i] = *reinterpret_cast<const Run4<Y>*>(y + max(fresh(row[s][i]), 0) * y_stride + (has_y ? m : 0));
+  };
+  // Whole steps, then what is left.  Rows of 2^k bytes begin in the same channel of the L2, and workgroups that walk along them in step would all
+  // want one: each begins somewhere else in its range.
+  const int first = m0 + 64 * wave, steps = first < m1 ? (m1 - 64 - first + 256) / 256 : 0;
+  const int begin = steps > 0 ? (int)(blockIdx.x * 3) % steps : 0;
+  auto m_of = [&](int i) {       // begin <= i; what is behind the last step is the last one again
+    const int k = min(i, begin + steps - 1);
+    return first + 256 * (k < steps ? k : k - steps);
+  };
   x8<T> w[F], next_w[F];
-  Run4<Y> before[4], next_before[4];
-  load_w(w, first, 0);
-  if (steps > 0) load_y(before, first);
-  // the parts of v
-  x8<T> vs[N][H == 0 ? 2 : H];
-  float factor[4];
+  Run4<Y> before[NS == 1 ? 2 : NS][4];           // of a step's rows (of this step's and the next's 16)
+  if (steps > 0) {
+    if (NS < 4) load_w(w, m_of(begin), 0);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) load_y(before[s], s, m_of(begin));
+  }
   {
-    const int splits = c.cut.splits(t.count, c.rows), left = rank - 8 * (H == 0 ? g & 1 : g);
-    const float* v = v_of(c, 0, blockIdx.y, p.at, sub) + (H == 0 ? (g & 1) * 16 + l16 : lane) * 8;
+    // The parts of v: 16 rows a wavefront, or of the same 16 a quarter of the sums' parts each.
+    constexpr bool ALL = NS == 1;
+    const int sub = ALL ? 0 : wave;
+    const int splits = c.cut.splits(t.count, c.rows), left = rank - 8 * (H == 0 ? g & 1 : g), halves = (p.max_rank + 31) / 32;
+    const float* v = v_of(c, 0, tile, p.at, sub0 + sub) + (H == 0 ? (g & 1) * 16 + l16 : lane) * 8;
     const int64_t v_split = (int64_t)c.v_tiles * c.cut.rank_halves * (4 * 512);
-    const int halves = (p.max_rank + 31) / 32;
+    const bool live = 16 * (sub0 + sub) + l16 < t.rows;
     f32x4 x[HV][2];
 #pragma unroll
     for (int h = 0; h < HV; ++h) x[h][0] = x[h][1] = f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8 / HV
-    for (int s = 0; s < splits; ++s)
+#pragma unroll 4 / HV
+    for (int s = ALL ? wave : sub < NS ? 0 : splits; s < splits; s += ALL ? 4 : 1)
 #pragma unroll
       for (int h = 0; h < HV; ++h) {
         const f32x4* from = reinterpret_cast<const f32x4*>(v + s * v_split + min(h, halves - 1) * (4 * 512));
         x[h][0] += from[0];
         x[h][1] += from[1];
       }
-    const bool live = 16 * sub + l16 < t.rows;
-    float top = 0.f, up = 1.f, mine = p.scale ? uniform(p.scale + t.slot) : 1.f;           // up: what the row is multiplied with
+    if (ALL) {
+#pragma unroll
+      for (int h0 = 0; h0 < HV; h0 += 2) {       // 64 ranks at a time
+        if (h0 > 0) __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (h0 + i / 2 < HV) sums[(4 * wave + i) * 64 + lane] = x[(h0 + i / 2) % HV][i % 2];
+        __syncthreads();
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (h0 + i / 2 < HV) {
+            f32x4 sum = sums[i * 64 + lane];
+#pragma unroll
+            for (int k = 1; k < 4; ++k) sum += sums[(4 * k + i) * 64 + lane];
+            x[(h0 + i / 2) % HV][i % 2] = sum;
+          }
+      }
+    }
+    float top = 0.f, up = 1.f, factor = p.scale ? uniform(p.scale + t.slot) : 1.f;         // up: what the row is multiplied with
 #pragma unroll
     for (int h = 0; h < HV; ++h)
 #pragma unroll
@@ -465,114 +494,136 @@ __device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, 
       top = fmaxf(top, __shfl_xor(top, 32));
       const int e = (int)(__float_as_uint(top) >> 23) - 127;                               // of its leading bit
       if (e < 128) up = __uint_as_float((uint32_t)(127 + 13 - max(e, -100)) << 23);
-      mine /= up;
+      factor /= up;
     }
+    if (ALL ? wave == 0 : sub < NS) {
+      if (lane < 16) factors[16 * sub + lane] = factor;
+      x8<T>* const to = vs + sub * (N * HL * 64) + lane;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) factor[i] = __shfl(mine, 4 * g + i);
+      for (int h = 0; h < HV; ++h) {
+        x8<T> piece[N];
 #pragma unroll
-    for (int h = 0; h < HV; ++h)
+        for (int e = 0; e < 8; ++e) {
+          float rest = x[h][e / 4][e % 4] * up;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        float rest = x[h][e / 4][e % 4] * up;
+          for (int part = 0; part < N; ++part) {
+            piece[part][e] = (T)rest;
+            rest -= (float)piece[part][e];
+          }
+        }
 #pragma unroll
         for (int part = 0; part < N; ++part) {
-          const T piece = (T)rest;
-          rest -= (float)piece;
           if (H == 0) {                          // for the operands' halves: ranks in the lower lanes, in the upper ones
-            vs[part][0][e] = g < 2 ? piece : (T)0.f;
-            vs[part][H == 0 ? 1 : 0][e] = g < 2 ? (T)0.f : piece;
+            to[(part * HL) * 64] = g < 2 ? piece[part] : x8<T>{};
+            to[(part * HL + HL - 1) * 64] = g < 2 ? x8<T>{} : piece[part];
           } else {
-            vs[part][h][e] = piece;
+            to[(part * HL + h) * 64] = piece[part];
           }
         }
       }
-  }
-  auto multiply = [&](f32x4 (&acc)[4], const x8<T> (&w)[F], int chunk) {
-    if (H == 0) {
-#pragma unroll
-      for (int part = 0; part < N; ++part)
-#pragma unroll
-        for (int j = 0; j < 4; ++j) acc[j] = mfma(vs[part][H == 0 ? j & 1 : 0], w[(j >> 1) % F], acc[j]);
-    } else {
-#pragma unroll
-      for (int h = 0; h < CH; ++h)
-#pragma unroll
-        for (int part = 0; part < N; ++part)
-#pragma unroll
-          for (int j = 0; j < 4; ++j) acc[j] = mfma(vs[part][(CH * chunk + h) % HV], w[(4 * h + j) % F], acc[j]);
     }
+    __syncthreads();
+  }
+  if (NS == 4 && steps > 0) load_w(w, m_of(begin), 0);
+  auto multiply = [&](f32x4 (&acc)[4], const x8<T> (&w)[F], int s, int chunk) {
+    const x8<T>* from = vs + s * (N * HL * 64) + lane;
+#pragma unroll
+    for (int h = 0; h < (H == 0 ? 1 : CH); ++h)
+#pragma unroll
+      for (int part = 0; part < N; ++part) {
+        if (H == 0) {
+          const x8<T> a = from[(part * HL) * 64], b = from[(part * HL + HL - 1) * 64];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = mfma(j & 1 ? b : a, w[(j >> 1) % F], acc[j]);
+        } else {
+          const x8<T> a = from[(part * HL + CH * chunk + h) * 64];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) acc[j] = mfma(a, w[(4 * h + j) % F], acc[j]);
+        }
+      }
   };
   auto zero = [](f32x4 (&acc)[4]) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) acc[j] = f32x4{0.f, 0.f, 0.f, 0.f};
   };
-  auto store = [&](const f32x4 (&acc)[4], const Run4<Y> (&before)[4], int m) {
+  auto store = [&](const f32x4 (&acc)[4], const Run4<Y> (&before)[4], int s, int m) {
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
+      const float f = factors[16 * s + 4 * g + i];
       Run4<Y> o;
 #pragma unroll
-      for (int j = 0; j < 4; ++j) o.e[j] = (Y)fmaf(factor[i], acc[j][i], has_y ? (float)before[i].e[j] : 0.f);
-      if (row[i] >= 0) *reinterpret_cast<Run4<Y>*>(static_cast<Y*>(p.out) + row[i] * p.out_stride + m + 4 * l16) = o;
+      for (int j = 0; j < 4; ++j) o.e[j] = (Y)fmaf(f, acc[j][i], has_y ? (float)before[i].e[j] : 0.f);
+      const int r = fresh(row[s][i]);
+      if (r >= 0) *reinterpret_cast<Run4<Y>*>(out + r * out_stride + m) = o;
     }
   };
-  auto step = [&](x8<T> (&w)[F], x8<T> (&next_w)[F], const Run4<Y> (&before)[4], Run4<Y> (&next_before)[4], int m, int next) {
-    f32x4 acc[4];
-    zero(acc);
-    load_y(next_before, next);
-    if (CHUNKS == 1) {
-      load_w(next_w, next, 0);
-      multiply(acc, w, 0);
-    } else {
+  // A step: its weights in w; at its end the next step's are in next_w (in w, where ranks come in chunks, and
+  // with 64 rows, whose elements of y need the registers).  turn: which of `before` has its 16 rows.
+  auto step = [&](x8<T> (&w)[F], x8<T> (&next_w)[F], int turn, int m, int next) {
+    if (CHUNKS == 1 && NS < 4) load_w(next_w, next, 0);
+    if (NS == 1) load_y(before[turn ^ 1], 0, next);
 #pragma unroll
-      for (int k = 0; k < CHUNKS; k += 2) {      // w: this chunk, next_w: the one after it
-        load_w(next_w, m, k + 1);
-        multiply(acc, w, k);
-        load_w(w, k + 2 < CHUNKS ? m : next, k + 2 < CHUNKS ? k + 2 : 0);
-        multiply(acc, next_w, k + 1);
+    for (int s = 0; s < NS; ++s) {
+      f32x4 acc[4];
+      zero(acc);
+      if (CHUNKS == 1) {
+        multiply(acc, w, s, 0);
+        if (NS == 4 && s + 1 == NS) load_w(w, next, 0);
+      } else {
+#pragma unroll
+        for (int k = 0; k < CHUNKS; k += 2) {    // w: this chunk, next_w: the one after it
+          load_w(next_w, m, k + 1);
+          multiply(acc, w, s, k);
+          const bool last = k + 2 >= CHUNKS;
+          load_w(w, last && s + 1 == NS ? next : m, last ? 0 : k + 2);
+          multiply(acc, next_w, s, k + 1);
+        }
       }
+      store(acc, before[NS == 1 ? turn : s], s, m);
+      if (NS > 1) load_y(before[s], s, next);
+      __builtin_amdgcn_sched_barrier(0);         // (what further rows need is not asked for here: registers)
     }
-    store(acc, before, m);
   };
-  int m = first;
-  const int end = first + stride * steps, behind = end - stride;                           // (behind the last step it is loaded again)
-  for (; m < end; m += 2 * stride) {
-    step(w, next_w, before, next_before, m, min(m + stride, behind));
-    if (m + stride >= end) break;
-    if (CHUNKS == 1) step(next_w, w, next_before, before, m + stride, min(m + 2 * stride, behind));
-    else step(w, next_w, next_before, before, m + stride, min(m + 2 * stride, behind));
+  for (int i = begin; i < begin + steps; i += 2) {
+    step(w, next_w, 0, m_of(i), m_of(i + 1));
+    if (i + 1 == begin + steps) break;
+    if (CHUNKS == 1 && NS < 4) step(next_w, w, 1, m_of(i + 1), m_of(i + 2));
+    else step(w, next_w, 1, m_of(i + 1), m_of(i + 2));
   }
-  if (end < m1) {
-    f32x4 acc[4];
-    zero(acc);
+  const int end = first + 256 * steps;
+  if (end < m1)
+    for (int s = 0; s < NS; ++s) {
+      f32x4 acc[4];
+      zero(acc);
 #pragma unroll
-    for (int k = 0; k < CHUNKS; ++k) {
-      load_w(w, end, k);
-      multiply(acc, w, k);
-    }
-#pragma unroll
-    for (int i = 0; i < 4; ++i)
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        const int at = end + 4 * l16 + j;
-        if (at < m1 && row[i] >= 0)
-          static_cast<Y*>(p.out)[row[i] * p.out_stride + at] = (Y)fmaf(factor[i], acc[j][i], has_y ? (float)y[i][end + j] : 0.f);
+      for (int k = 0; k < CHUNKS; ++k) {
+        load_w(w, end, k);
+        multiply(acc, w, s, k);
       }
-  }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const int r = __shfl(t.row, 16 * (sub0 + s) + 4 * g + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+          if (end + 4 * l16 + j < m1 && r >= 0)
+            out[r * out_stride + end + j] = (Y)fmaf(factors[16 * s + 4 * g + i], acc[j][i], has_y ? (float)y[r * y_stride + end + j] : 0.f);
+      }
+    }
 }
 
-// Rows that no adapter changes: a wavefront takes 256 elements of a row, four such pieces on their way at once.
+// Rows that no adapter changes: a wavefront takes 256 elements of a row, eight such pieces on their way at once.
 template <typename Y>
 __device__ __forceinline__ void copy_rows(const Projection& p, const Tile& t, int m0, int m1) {
   const Y* y = static_cast<const Y*>(p.y);
   Y* out = static_cast<Y*>(p.out);
   if (y == out && p.y_stride == p.out_stride) return;
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), pieces = t.rows * ((m1 - m0 + 255) / 256);
-  for (int i0 = wave; i0 < pieces; i0 += 16) {
-    Run4<Y> x[4];
-    int64_t row[4];
-    int m[4];
+  for (int i0 = wave; i0 < pieces; i0 += 32) {
+    Run4<Y> x[8];
+    int64_t row[8];
+    int m[8];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < 8; ++i) {
       const int piece = min(i0 + 4 * i, pieces - 1);
       row[i] = __shfl(t.row, piece % t.rows);
       m[i] = m0 + 256 * (piece / t.rows) + 4 * lane;
@@ -585,7 +636,7 @@ __device__ __forceinline__ void copy_rows(const Projection& p, const Tile& t, in
         for (int e = 0; e < 4; ++e) x[i].e[e] = y[at + min(m[i] + e, m1 - 1)];
     }
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < 8; ++i)
       if (row[i] >= 0) {
         Y* to = out + row[i] * p.out_stride + m[i];
         if (m[i] + 4 <= m1) *reinterpret_cast<Run4<Y>*>(to) = x[i];
@@ -597,21 +648,49 @@ __device__ __forceinline__ void copy_rows(const Projection& p, const Tile& t, in
   }
 }
 
-// LONG: ranks above 64.
-template <typename T, typename Y, bool LONG>
-__global__ void __launch_bounds__(256) expand_kernel(Call c) {
-  const Projection& p = c.p[blockIdx.z];
-  const int m0 = c.span * (int)blockIdx.x, m1 = min(p.m, m0 + c.span);
-  if (m0 >= m1) return;
-  const Tile t = tile_at(c, blockIdx.y);
-  if (t.rows == 0) return;
-  const int rank = rank_of(p, t.slot);
-  if (rank <= 0) copy_rows<Y>(p, t, m0, m1);
-  else if (p.max_rank <= 16) expand_rows<T, Y, 0>(c, p, t, rank, m0, m1);
-  else if (rank <= 32) expand_rows<T, Y, 1>(c, p, t, rank, m0, m1);
-  else if (!LONG || rank <= 64) expand_rows<T, Y, 2>(c, p, t, rank, m0, m1);
-  else if (rank <= 128) expand_rows<T, Y, LONG ? 4 : 2>(c, p, t, rank, m0, m1);
-  else expand_rows<T, Y, LONG ? 8 : 2>(c, p, t, rank, m0, m1);
+// The outputs' rows lie in a line, tile after tile, projection after projection, 256 elements a piece; a workgroup takes an equal part of it, as long as
+// no projection of a tile ends.  (A grid of pieces of 1024: the last ones leave half of the card idle, 150 us in place of XX for adapt-prompts.)
+// KIND: steps of up to 16 rows (registers for twice the workgroups), any rows, ranks above 64.
+enum Kind { kFew, kAny, kLong };
+template <typename T, typename Y, Kind KIND>
+__global__ void __launch_bounds__(256, KIND == kLong ? 1 : KIND == kAny ? 2 : 3) expand_kernel(Call c) {
+  constexpr bool LONG = KIND == kLong;
+  constexpr int N = Parts<T>::N;
+  __shared__ f32x4 sums[16 * 64];
+  __shared__ x8<T> vs[N * 8 * 64];               // 64 rows of 64 ranks, or 16 of 256
+  __shared__ float factors[kTile];
+  const unsigned pieces = min(uniform(c.count), c.max_tiles) * c.pieces, each = pieces / gridDim.x, more = pieces % gridDim.x;
+  unsigned at = each * blockIdx.x + min(blockIdx.x, more);
+  const unsigned end = at + each + (blockIdx.x < more);
+  while (at < end) {
+    int piece = (int)(at % c.pieces), which = 0;
+    const int tile = (int)(at / c.pieces);
+    for (; piece >= (c.p[which].m + 255) / 256; ++which) piece -= (c.p[which].m + 255) / 256;
+    const Projection& p = c.p[which];
+    const int run = (int)min(end - at, (unsigned)((p.m + 255) / 256 - piece)), m0 = 256 * piece, m1 = min(p.m, m0 + 256 * run);
+    at += run;
+    const Tile t = tile_at(c, tile);
+    if (t.rows == 0) continue;
+    const int rank = rank_of(p, t.slot);
+    if (rank <= 0) {
+      copy_rows<Y>(p, t, m0, m1);
+      continue;
+    }
+    __syncthreads();                             // everyone is done with the last rows
+#define SPQR_EXPAND(H, NS, SUB) expand_rows<T, Y, H, NS>(c, p, t, tile, SUB, rank, m0, m1, sums, vs, factors)
+#define SPQR_EXPAND_ROWS(H) do { if (KIND == kFew || t.rows <= 16) SPQR_EXPAND(H, 1, 0); else if (t.rows <= 32) SPQR_EXPAND(H, 2, 0); else SPQR_EXPAND(H, 4, 0); } while (0)
+    if (LONG && rank > 64) {
+      for (int sub = 0; 16 * sub < t.rows; ++sub) {
+        if (sub > 0) __syncthreads();
+        if (rank <= 128) SPQR_EXPAND(LONG ? 4 : 2, 1, sub);
+        else SPQR_EXPAND(LONG ? 8 : 2, 1, sub);
+      }
+    } else if (p.max_rank <= 16) SPQR_EXPAND_ROWS(0);
+    else if (rank <= 32) SPQR_EXPAND_ROWS(1);
+    else SPQR_EXPAND_ROWS(2);
+#undef SPQR_EXPAND_ROWS
+#undef SPQR_EXPAND
+  }
 }
 
 static int check_bank(const spqr_adapters_t* a) {
@@ -651,30 +730,30 @@ static Call call_of(const spqr_adapters_t* a, const spqr_adapter_plan_t* plan, i
 }
 
 template <typename T, typename Y>
-static void launch_expand(const Call& c, bool longer, dim3 grid, hipStream_t st) {
-  if (longer) hipLaunchKernelGGL((expand_kernel<T, Y, true>), grid, dim3(256), 0, st, c);
-  else hipLaunchKernelGGL((expand_kernel<T, Y, false>), grid, dim3(256), 0, st, c);
+static void launch_expand(const Call& c, bool longer, int pieces, hipStream_t st) {
+  // as many workgroups as the card's registers have room for
+  if (longer) hipLaunchKernelGGL((expand_kernel<T, Y, kLong>), dim3(min(pieces, 256)), dim3(256), 0, st, c);
+  else if (c.rows <= 16) hipLaunchKernelGGL((expand_kernel<T, Y, kFew>), dim3(min(pieces, 768)), dim3(256), 0, st, c);
+  else hipLaunchKernelGGL((expand_kernel<T, Y, kAny>), dim3(min(pieces, 512)), dim3(256), 0, st, c);
 }
 
 template <typename T>
 static int launch_adapters(Call& c, int count, int y_dtype, int tiles, hipStream_t st) {
-  int most = 0, groups = 0;
-  int64_t all = 0;
+  int groups = 0;
   bool longer = false;
+  c.pieces = 0;
   for (int p = 0; p < count; ++p) {
-    most = c.p[p].m > most ? c.p[p].m : most;
-    all += (c.p[p].m + 255) / 256;
+    c.pieces += (c.p[p].m + 255) / 256;
     groups += (c.p[p].max_rank + 16 * kWaveTiles - 1) / (16 * kWaveTiles);
     longer = longer || c.p[p].max_rank > 64;
   }
-  const int64_t rounds = all * tiles / kExpandGroups;
-  c.span = 256 * (int)(rounds < 1 ? 1 : rounds < kMostRounds ? rounds : kMostRounds);
-  // Workgroups for the most tiles and parts that there can be, and for the widest output; those that are too many end at once.
-  const dim3 shrink(c.cut.splits(1, c.rows), tiles, groups), expand((most + c.span - 1) / c.span, tiles, count);
+  // Workgroups for the most tiles and parts that there can be; those that are too many end at once.
+  const dim3 shrink(c.cut.splits(1, c.rows), tiles, groups);
+  const int pieces = tiles * c.pieces;           // 20481 tiles of 2048 pieces at most
   hipLaunchKernelGGL((shrink_kernel<T>), shrink, dim3(256), 0, st, c);
-  if (y_dtype == SPQR_F32) launch_expand<T, float>(c, longer, expand, st);
-  else if (y_dtype == SPQR_F16) launch_expand<T, _Float16>(c, longer, expand, st);
-  else launch_expand<T, __bf16>(c, longer, expand, st);
+  if (y_dtype == SPQR_F32) launch_expand<T, float>(c, longer, pieces, st);
+  else if (y_dtype == SPQR_F16) launch_expand<T, _Float16>(c, longer, pieces, st);
+  else launch_expand<T, __bf16>(c, longer, pieces, st);
   return launched();
 }
 
