@@ -3,24 +3,265 @@
 
 namespace spqr_blk {
 
-// Sum over the `lanes` threads of a row (a power of two; whole wavefronts above 64), in every one of them.  part: one float a
-// wavefront; all threads of the workgroup take part.
-__device__ __forceinline__ float row_sum(float v, int lanes, float* part) {
-  for (int d = min(lanes, 64) >> 1; d > 0; d >>= 1) v += __shfl_xor(v, d);
-  if (lanes > 64) {
-    const int wave = threadIdx.x >> 6, waves = lanes >> 6, first = wave & ~(waves - 1);
-    __syncthreads();                             // everyone has read the last sum
-    if ((threadIdx.x & 63) == 0) part[wave] = v;
-    __syncthreads();
-    v = 0.f;
-    for (int w = 0; w < waves; ++w) v += part[first + w];
+using spqr::wave_allreduce;
+
+// Sum over the `lanes` threads of a row (a power of two; whole wavefronts above 64), in every one of them.  part: two buffers of one float a
+// wavefront, taken in turn, so that one barrier a sum is enough (the next sum's stands between its readers and the next writers).
+struct RowSum {
+  float (*part)[16];
+  int lanes, turn;
+  __device__ __forceinline__ float operator()(float v) {
+    const int lane = threadIdx.x & 63;
+    if (lanes < 64) {
+      for (int d = lanes >> 1; d > 0; d >>= 1) v += __shfl_xor(v, d);
+      return v;
+    }
+    v = wave_allreduce(v, lane);
+    if (lanes > 64) {
+      const int wave = threadIdx.x >> 6, waves = lanes >> 6, first = wave & ~(waves - 1);
+      if (lane == 0) part[turn][wave] = v;
+      __syncthreads();
+      if (waves == 2) {
+        v = part[turn][first] + part[turn][first + 1];
+      } else {
+        v = 0.f;
+#pragma unroll
+        for (int w = 0; w < 16; w += 4)          // (all are asked for at once)
+          if (w < waves) {
+            const float4 f = *reinterpret_cast<const float4*>(&part[turn][first + w]);
+            v += (f.x + f.y) + (f.z + f.w);
+          }
+      }
+      turn ^= 1;
+    }
+    return v;
   }
-  return v;
+};
+
+__device__ __forceinline__ float activated(int act, float g) {
+  if (act == SPQR_ACT_TANH) return tanhf(g);
+  const float s = __builtin_amdgcn_rcpf(1.f + __expf(-g));
+  return act == SPQR_ACT_SIGMOID ? s : g * s;
 }
 
+// ---------------------------------------------------------------------------------------------------------------------
+// Rows of up to 8192 elements: eight of them a thread.
+// ---------------------------------------------------------------------------------------------------------------------
+// Eight elements as they were loaded, of any type: they are worked out where they are needed, so that the loads of all terms are on their
+// way at once.
+struct Raw { u32x4 a, b; };
+typedef u32x4 u32x4_at2 __attribute__((aligned(2)));
+
+__device__ __forceinline__ void load(Raw& r, int dtype, const void* p, int64_t element) {
+  const char* at = static_cast<const char*>(p) + element * (dtype == SPQR_F32 ? 4 : 2);
+  r.a = *reinterpret_cast<const u32x4_at2*>(at);
+  if (dtype == SPQR_F32) r.b = *reinterpret_cast<const u32x4_at2*>(at + 16);
+}
+__device__ __forceinline__ void floats(const Raw& r, int dtype, float (&v)[8]) {
+  if (dtype == SPQR_F32) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e < 4 ? r.a[e] : r.b[e - 4]);
+  } else if (dtype == SPQR_F16) {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = spqr::h2f((uint16_t)(r.a[e / 2] >> 16 * (e & 1)));
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; ++e) v[e] = __uint_as_float(e & 1 ? r.a[e / 2] & 0xFFFF0000u : r.a[e / 2] << 16);
+  }
+}
+
+// Where a thread's eight elements lie in a row: it reads those from `from` on, whatever it has; `shift` of them are another thread's where the row
+// ends inside its eight, `count` (0 .. 8) are there.  ODD: rows whose length is no multiple of 8; else a thread has all eight or none.
+struct Place { int col, from, shift, count; };
+
+template <bool ODD>
+__device__ __forceinline__ void floats_at(const Raw& r, int dtype, const Place& at, float (&v)[8]) {
+  floats(r, dtype, v);
+  if (!ODD) return;
+#pragma unroll
+  for (int d = 4; d > 0; d >>= 1)
+#pragma unroll
+    for (int e = 0; e + d < 8; ++e) v[e] = at.shift & d ? v[e + d] : v[e];
+}
+// What is no element counts nothing.
+template <bool ODD, int CH>
+__device__ __forceinline__ float sum_of(const float (&v)[CH][8], const Place (&at)[CH]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) s += !ODD || e < at[c].count ? v[c][e] : 0.f;
+    sum += ODD || at[c].count > 0 ? s : 0.f;
+  }
+  return sum;
+}
+template <bool ODD, int CH>
+__device__ __forceinline__ float squares_of(const float (&v)[CH][8], const Place (&at)[CH]) {
+  float sum = 0.f;
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float s = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      const float x = !ODD || e < at[c].count ? v[c][e] : 0.f;
+      s = fmaf(x, x, s);
+    }
+    sum += ODD || at[c].count > 0 ? s : 0.f;
+  }
+  return sum;
+}
+
+template <bool ODD, int CH>
+__device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Place (&at)[CH], const spqr_residual_norm_t& p, const void* weight, const void* bias,
+                                          const Raw (&w)[CH], const Raw (&b)[CH], RowSum& sum) {
+  if (kind == SPQR_NORM_NONE) return;
+  const float inverse = 1.f / (float)p.width;
+  if (kind == SPQR_NORM_LAYER) {
+    const float mean = sum(sum_of<ODD>(v, at)) * inverse;
+#pragma unroll
+    for (int c = 0; c < CH; ++c)
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] -= mean;
+  }
+  const float r = 1.f / sqrtf(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    float x[8], y[8];
+    if (weight) {
+      floats_at<ODD>(w[c], p.weight_dtype, at[c], x);
+      if (p.weight_offset != 0.f)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) x[e] += p.weight_offset;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] *= r * x[e];
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] *= r;
+    }
+    if (bias) {
+      floats_at<ODD>(b[c], p.weight_dtype, at[c], y);
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[c][e] += y[e];
+    }
+  }
+}
+
+template <typename T> struct TypeOf { static constexpr int value = SPQR_F32; };
+template <> struct TypeOf<_Float16> { static constexpr int value = SPQR_F16; };
+template <> struct TypeOf<__bf16> { static constexpr int value = SPQR_BF16; };
+
+// `lanes` threads a row, rows in turn; the next row's terms are on their way while one is worked out.
+template <typename X, typename Y, bool ODD, int CH>
+__global__ void __launch_bounds__(1024 / CH) norm_rows_kernel(spqr_residual_norm_t p, int lanes) {
+  __shared__ __align__(16) float part[2][16];
+  constexpr int XT = TypeOf<X>::value, YT = TypeOf<Y>::value;
+  const int n = p.width, in_row = threadIdx.x & (lanes - 1), per = blockDim.x / lanes, mine = threadIdx.x / lanes;
+  const bool has_x = p.x != nullptr, has_y = p.y != nullptr, has_gate = p.gate != nullptr;
+  Place at[CH];
+#pragma unroll
+  for (int c = 0; c < CH; ++c) {
+    at[c].col = 8 * (in_row + lanes * c);
+    at[c].count = min(max(n - at[c].col, 0), 8);
+    at[c].from = min(at[c].col, n - 8);
+    at[c].shift = at[c].count > 0 ? at[c].col - at[c].from : 0;
+  }
+  RowSum sum{part, lanes, 0};
+  int64_t first = (int64_t)blockIdx.x * per, t = min(first + mine, (int64_t)p.rows - 1);
+  Raw y[CH], x[CH], g[CH];
+  auto load_row = [&](int64_t t, bool gate) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if (has_y) load(y[c], YT, p.y, t * p.y_stride + at[c].from);
+      if (has_x) load(x[c], XT, p.x, t * p.x_stride + at[c].from);
+      if (gate) load(g[c], p.gate_dtype, p.gate, t * p.gate_stride + at[c].from);
+    }
+  };
+  auto load_vectors = [&](Raw (&w)[CH], Raw (&b)[CH], const void* weight, const void* bias) {
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if (weight) load(w[c], p.weight_dtype, weight, at[c].from);
+      if (bias) load(b[c], p.weight_dtype, bias, at[c].from);
+    }
+  };
+  load_row(t, has_gate);
+  for (; first < p.rows; first += (int64_t)gridDim.x * per) {
+    const bool live = first + mine < p.rows;     // (other threads take part in the sums, and store nothing)
+    const int64_t here = t;
+    float v[CH][8], xs[CH][8], f[CH][8];
+    Raw w[CH], b[CH];
+    load_vectors(w, b, p.y_weight, p.y_bias);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if (has_y) floats_at<ODD>(y[c], YT, at[c], v[c]);
+      if (has_x) floats_at<ODD>(x[c], XT, at[c], xs[c]);
+      if (has_gate) floats_at<ODD>(g[c], p.gate_dtype, at[c], f[c]);
+    }
+    const int64_t next = first + (int64_t)gridDim.x * per;
+    if (next < p.rows) {
+      t = min(next + mine, (int64_t)p.rows - 1);
+      load_row(t, has_gate && p.gate_stride != 0);
+    }
+    if (has_y) {
+      norm_rows<ODD>(p.norm_y, v, at, p, p.y_weight, p.y_bias, w, b, sum);
+#pragma unroll
+      for (int c = 0; c < CH; ++c) {
+        if (has_gate) {
+          if (p.act != SPQR_ACT_NONE)
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[c][e] = activated(p.act, f[c][e]);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) v[c][e] *= f[c][e];
+        }
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] *= p.scale;
+      }
+    }
+    load_vectors(w, b, p.x_weight, p.x_bias);
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if (has_x)
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[c][e] = has_y ? fmaf(p.skip, xs[c][e], v[c][e]) : p.skip * xs[c][e];
+      if (p.sum && live && at[c].count > 0) store_row8_as(XT, p.sum, here * p.sum_stride, at[c].col, n, v[c]);
+    }
+    if (p.out) {
+      norm_rows<ODD>(p.norm_x, v, at, p, p.x_weight, p.x_bias, w, b, sum);
+#pragma unroll
+      for (int c = 0; c < CH; ++c)
+        if (live && at[c].count > 0) store_row8_as(p.out_dtype, p.out, here * p.out_stride, at[c].col, n, v[c]);
+    }
+  }
+}
+
+constexpr int64_t kThreads = 512 * 1024;         // as many as run at once
+
+template <typename X, typename Y, bool ODD>
+static void launch_rows(const spqr_residual_norm_t& p, int lanes, int threads, int64_t groups, hipStream_t st) {
+  const int64_t most = kThreads / threads;
+  const dim3 grid((unsigned)(groups < most ? groups : most));
+  hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, 1>), grid, dim3(threads), 0, st, p, lanes);
+}
+
+template <typename X, bool ODD>
+static void launch_rows_of(const spqr_residual_norm_t& p, int lanes, int threads, int64_t groups, hipStream_t st) {
+  if (!p.y || p.y_dtype == SPQR_F32) launch_rows<X, float, ODD>(p, lanes, threads, groups, st);
+  else if (p.y_dtype == SPQR_F16) launch_rows<X, _Float16, ODD>(p, lanes, threads, groups, st);
+  else launch_rows<X, __bf16, ODD>(p, lanes, threads, groups, st);
+}
+
+template <typename X>
+static void launch_rows_any(const spqr_residual_norm_t& p, int lanes, int threads, int64_t groups, hipStream_t st) {
+  if (p.width % 8 == 0) launch_rows_of<X, false>(p, lanes, threads, groups, st);
+  else launch_rows_of<X, true>(p, lanes, threads, groups, st);
+}
+
+// ---------------------------------------------------------------------------------------------------------------------
+// Longer rows, and rows of fewer than eight elements.
+// ---------------------------------------------------------------------------------------------------------------------
 template <int CH>
 __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at)[CH], int n, float eps, int weight_dtype, float offset,
-                                     const void* weight, const void* bias, int lanes, float* part) {
+                                     const void* weight, const void* bias, RowSum& row_sum) {
   if (kind == SPQR_NORM_NONE) return;
   float mean = 0.f;
   if (kind == SPQR_NORM_LAYER) {
@@ -29,7 +270,7 @@ __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at
     for (int c = 0; c < CH; ++c)
 #pragma unroll
       for (int e = 0; e < 8; ++e) sum += v[c][e];
-    mean = row_sum(sum, lanes, part) / (float)n;
+    mean = row_sum(sum) / (float)n;
   }
   float squares = 0.f;
 #pragma unroll
@@ -39,7 +280,7 @@ __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at
       v[c][e] = at[c] + e < n ? v[c][e] - mean : 0.f;
       squares = fmaf(v[c][e], v[c][e], squares);
     }
-  const float r = 1.f / sqrtf(row_sum(squares, lanes, part) / (float)n + eps);
+  const float r = 1.f / sqrtf(row_sum(squares) / (float)n + eps);
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     float w[8], b[8];
@@ -53,19 +294,15 @@ __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at
     if (bias && at[c] < n) load_row8_as(weight_dtype, bias, 0, at[c], n, b);
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[c][e] = fmaf(v[c][e] * r, w[e], b[e]);
+    if (CH > 2) __builtin_amdgcn_sched_barrier(0);         // (registers)
   }
-}
-
-__device__ __forceinline__ float activated(int act, float g) {
-  if (act == SPQR_ACT_TANH) return tanhf(g);
-  const float s = 1.f / (1.f + __expf(-g));
-  return act == SPQR_ACT_SIGMOID ? s : g * s;
 }
 
 // `lanes` threads a row, CH runs of eight elements each, which stay in registers from the loads to the stores.
 template <int CH>
 __global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_t p, int lanes) {
-  __shared__ float part[16];
+  __shared__ __align__(16) float part[2][16];
+  RowSum row_sum{part, lanes, 0};
   const int n = p.width, in_row = threadIdx.x & (lanes - 1);
   const int64_t row = (int64_t)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
   const bool live = row < p.rows;
@@ -80,7 +317,7 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_
     if (p.y && at[c] < n) load_row8_as(p.y_dtype, p.y, t * p.y_stride, at[c], n, v[c]);
   }
   if (p.y) {
-    norm<CH>(p.norm_y, v, at, n, p.eps, p.weight_dtype, p.weight_offset, p.y_weight, p.y_bias, lanes, part);
+    norm<CH>(p.norm_y, v, at, n, p.eps, p.weight_dtype, p.weight_offset, p.y_weight, p.y_bias, row_sum);
 #pragma unroll
     for (int c = 0; c < CH; ++c) {
       float g[8];
@@ -94,6 +331,7 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_
       }
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] *= p.scale;
+      if (CH > 2) __builtin_amdgcn_sched_barrier(0);
     }
   }
 #pragma unroll
@@ -107,9 +345,10 @@ __global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_
 #pragma unroll
     for (int e = 0; e < 8; ++e) v[c][e] = at[c] + e < n ? v[c][e] : 0.f;
     if (p.sum && live && at[c] < n) store_row8_as(p.x_dtype, p.sum, t * p.sum_stride, at[c], n, v[c]);
+    if (CH > 2) __builtin_amdgcn_sched_barrier(0);
   }
   if (!p.out) return;
-  norm<CH>(p.norm_x, v, at, n, p.eps, p.weight_dtype, p.weight_offset, p.x_weight, p.x_bias, lanes, part);
+  norm<CH>(p.norm_x, v, at, n, p.eps, p.weight_dtype, p.weight_offset, p.x_weight, p.x_bias, row_sum);
 #pragma unroll
   for (int c = 0; c < CH; ++c)
     if (live && at[c] < n) store_row8_as(p.out_dtype, p.out, t * p.out_stride, at[c], n, v[c]);
@@ -160,6 +399,12 @@ extern "C" int spqr_residual_norm(const spqr_residual_norm_t* p, void* stream) {
   const dim3 g((unsigned)grid), b(threads);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int ch = (runs + lanes - 1) / lanes;
+  if (ch <= 1 && p->width >= 8) {
+    if ((!p->x && !p->sum) || p->x_dtype == SPQR_F32) launch_rows_any<float>(*p, lanes, threads, grid, st);
+    else if (p->x_dtype == SPQR_F16) launch_rows_any<_Float16>(*p, lanes, threads, grid, st);
+    else launch_rows_any<__bf16>(*p, lanes, threads, grid, st);
+    return launched();
+  }
   if (ch <= 1) hipLaunchKernelGGL(residual_norm_kernel<1>, g, b, 0, st, *p, lanes);
   else if (ch <= 2) hipLaunchKernelGGL(residual_norm_kernel<2>, g, b, 0, st, *p, lanes);
   else if (ch <= 4) hipLaunchKernelGGL(residual_norm_kernel<4>, g, b, 0, st, *p, lanes);
