@@ -184,10 +184,15 @@ def test_scores_of_nothing():
 
 
 def test_scores_refuse_a_workspace_that_is_none():
-    need = K._lib().spqr_token_logprobs_workspace_bytes(C.byref(scores_of()))
-    assert need >= 0
-    if need:
-        assert score(workspace=None) == NULL and score(workspace=SOME + 128) == ALIGN and score(workspace_bytes=need - 1) == WORKSPACE
+    """Rows that are cut into parts need one; no fewer bytes for more rows."""
+    lib = K._lib()
+    bytes_of = lambda **change: lib.spqr_token_logprobs_workspace_bytes(C.byref(scores_of(**change)))  # noqa: E731
+    assert bytes_of() == 0 and bytes_of(rows=100000) == 0
+    got = [bytes_of(rows=n, vocab=100000, top=64) for n in (0, 1, 2, 7, 100, 512, 513, 5000)]
+    assert got == sorted(got) and got[0] == 0 and got[1] > 0 and all(b % 256 == 0 for b in got)
+    for rows in (1, 3, 40):
+        wide = dict(rows=rows, vocab=100000, stride=100000)
+        assert score(workspace=None, **wide) == NULL and score(workspace=SOME + 128, **wide) == ALIGN and score(workspace_bytes=0, **wide) == WORKSPACE
 
 
 def test_handles_refuse_what_is_not_on_the_card():
