@@ -60,17 +60,35 @@ __device__ __forceinline__ void load_logits(const T* row, int at, int n, float (
       if (at + e >= n) v[e] = -INFINITY;
 }
 
+// log2 of a positive number: of its significand, near 1, by the card's instruction (off by 2^-23 or so), and its exponent.
+__device__ __forceinline__ double log2_of(float x) {
+  int e;
+  float m = frexpf(x, &e);                       // 0.5 .. 1
+  if (m < 0.70710678f) { m *= 2.f; --e; }
+  return (double)e + (double)__builtin_amdgcn_logf(m);
+}
+
+// A number that the k-th largest of a wavefront's 64 is not below, and no more than its last 12 bits under it: bit by bit, by how many reach it.  (A
+// loop of few instructions: code that runs once waits for its own instructions, 64 comparisons written out took 2 us more.)
+__device__ __forceinline__ uint32_t kth_largest(uint32_t key, int k) {
+  uint32_t bound = 0;
+#pragma unroll 1
+  for (uint32_t bit = 0x80000000u; bit >= 0x1000u; bit >>= 1)
+    if (__popcll(__ballot(key >= (bound | bit))) >= k) bound |= bit;
+  return bound;
+}
+
 // What is written of a row, once its sums are known: l c was rounded alike in all of them, so that it is differences from the largest logit
 // that count, and that one's own come from the scale itself.
 struct Row {
   Part soft;
   double scale, log_sum;                         // of 2^((l - max) c)
   __device__ __forceinline__ Row(const Part& p, float s)
-      : soft(p), scale(s), log_sum(p.sum == 0.f ? 0.0 : log2((double)p.sum) + (p.ref - (double)p.max * (s * kLog2e))) {}
+      : soft(p), scale(s), log_sum(p.sum == 0.f ? 0.0 : log2_of(p.sum) + (p.ref - (double)p.max * (s * kLog2e))) {}
   __device__ __forceinline__ float logprob(float x) const {
     return soft.sum == 0.f ? -INFINITY : (float)(((double)x - soft.max) * scale - log_sum * kLn2);
   }
-  __device__ __forceinline__ float entropy() const { return soft.sum == 0.f ? 0.f : (float)((log2((double)soft.sum) - (double)soft.dot / soft.sum) * kLn2); }
+  __device__ __forceinline__ float entropy() const { return soft.sum == 0.f ? 0.f : (float)((log2_of(soft.sum) - (double)soft.dot / soft.sum) * kLn2); }
 };
 
 template <typename T>
@@ -197,13 +215,8 @@ __global__ void __launch_bounds__(NT) score_kernel(spqr_token_logprobs_t p, int 
     float g = maxima[lane];
 #pragma unroll
     for (int w = 1; w < WAVES; ++w) g = fmaxf(g, maxima[64 * w + lane]);
-    int rank = 0;
-#pragma unroll
-    for (int i = 0; i < 64; ++i) {
-      const float o = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), i));
-      rank += o > g || (o == g && i < lane);
-    }
-    bound = __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(g), __ffsll(__ballot(rank == k - 1)) - 1));
+    const uint32_t key = kth_largest(ordered(g), k);
+    bound = key <= 0x007FFFFFu ? -INFINITY : unordered(key);                              // (0x007FFFFF: -infinity; below it are no numbers)
     if (mine >= bound && mine > -INFINITY)
       for (int i = 8 * tid; i < n; i += 8 * NT) {
         float v[8];
@@ -289,14 +302,7 @@ __global__ void __launch_bounds__(256) score_join_kernel(spqr_token_logprobs_t p
   uint64_t g = maxima[lane];
 #pragma unroll
   for (int w = 1; w < 4; ++w) g = maxima[64 * w + lane] > g ? maxima[64 * w + lane] : g;
-  int rank = 0;
-#pragma unroll
-  for (int i = 0; i < 64; ++i) {
-    const uint64_t o = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(g >> 32), i) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)g, i);
-    rank += o > g || (o == g && i < lane);       // (0, no key, more than once)
-  }
-  const int at = __ffsll(__ballot(rank == k - 1)) - 1;
-  const uint64_t bound = (uint64_t)(uint32_t)__builtin_amdgcn_readlane((uint32_t)(g >> 32), at) << 32 | (uint32_t)__builtin_amdgcn_readlane((uint32_t)g, at);
+  const uint64_t bound = (uint64_t)kth_largest((uint32_t)(g >> 32), k) << 32;
 #pragma unroll
   for (int i = 0; i < kJoined / 256; ++i)
     if (mine[i] != 0 && mine[i] >= bound) cand[atomicAdd(&found, 1)] = mine[i];
@@ -308,11 +314,9 @@ __global__ void __launch_bounds__(256) score_join_kernel(spqr_token_logprobs_t p
 
 // How many parts a row is cut into, and how long they are.
 struct Cut { int parts, length; };
-#include <stdlib.h>
-static int knob(const char* n, int d) { const char* v = getenv(n); return v ? atoi(v) : d; }
 static Cut cut_of(int64_t rows, int vocab, int top) {
-  int64_t parts = rows > 0 ? knob("KP",512) / rows : 1;
-  const int64_t by_length = (vocab + knob("KS",4096) - 1) / knob("KS",4096), by_keys = top > 0 ? kJoined / top : 64;
+  int64_t parts = rows > 0 ? kPartGroups / rows : 1;
+  const int64_t by_length = (vocab + kShortest - 1) / kShortest, by_keys = top > 0 ? kJoined / top : 64;
   if (parts > by_length) parts = by_length;
   if (parts > by_keys) parts = by_keys;
   if (parts > 64) parts = 64;
@@ -334,8 +338,7 @@ static int launch_score(const spqr_token_logprobs_t& p, hipStream_t st) {
   Part* parts = static_cast<Part*>(p.workspace);
   uint64_t* keys = reinterpret_cast<uint64_t*>(parts + (int64_t)p.rows * cut.parts);
   if (cut.parts == 1) {
-    if (knob("NT",0) == 1024) hipLaunchKernelGGL((score_kernel<T, 1024, true>), dim3(p.rows), dim3(1024), 0, st, p, p.vocab, nullptr, nullptr);
-    else if (p.vocab <= 8192 || knob("NT",0)==256) hipLaunchKernelGGL((score_kernel<T, 256, true>), dim3(p.rows), dim3(256), 0, st, p, p.vocab, nullptr, nullptr);
+    if (p.vocab <= 8192) hipLaunchKernelGGL((score_kernel<T, 256, true>), dim3(p.rows), dim3(256), 0, st, p, p.vocab, nullptr, nullptr);
     else hipLaunchKernelGGL((score_kernel<T, 512, true>), dim3(p.rows), dim3(512), 0, st, p, p.vocab, nullptr, nullptr);
     return launched();
   }
