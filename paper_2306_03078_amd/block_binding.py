@@ -6,6 +6,7 @@ runs in the library's kernels.  No CPU fallback: a missing libspqr.so raises.  A
 from __future__ import annotations
 
 import ctypes as C
+from struct import Struct
 
 from . import binding as B
 from . import serve_binding as S
@@ -46,11 +47,19 @@ class spqr_token_logprobs_t(C.Structure):
 
 
 _entry = {}
+_empty = _empty_like = _float32 = None                      # torch's
+# What a call changes of a descriptor, written at once: a field at a time costs as much as the launch.
+_norm_types, _norm_rows = Struct("=6i"), Struct("=10q")     # rows .. out_dtype (width among them); x .. out, x_stride .. gate_stride
+_norm_rows_at = spqr_residual_norm_t.x.offset
+_bank_rows, _bank_rows_at = Struct("=%dq" % (4 * SPQR_MAX_FUSED)), spqr_adapters_t.y.offset      # y, out, y_stride, out_stride
 
 
 def _lib():
+    global _empty, _empty_like, _float32
     lib = S._lib()
     if not _entry:
+        import torch
+        _empty, _empty_like, _float32 = torch.empty, torch.empty_like, torch.float32
         for name, rest in (("spqr_residual_norm", [_vp]), ("spqr_adapter_plan", [_vp]), ("spqr_adapters", [_vp, _vp]), ("spqr_token_logprobs", [_vp])):
             f = getattr(lib, name)
             f.restype, f.argtypes = C.c_int, [_vp] + rest
@@ -84,9 +93,9 @@ def _device(device):
 
 def _stride(name, t, shape, index, dtype=None):
     """Elements between the rows of t, which has this shape, contiguous rows, and this type (None: any of the three)."""
+    row, inner = t.stride() if t.dim() == 2 else (0, 0)
     if t.shape != shape or t.get_device() != index or (t.dtype not in S._dtypes if dtype is None else t.dtype != dtype):
         raise ValueError(f"{name}: {dtype or 'float32, float16 or bfloat16'} {list(shape)} on cuda:{index}, not {t.dtype} {list(t.shape)} on {t.device}")
-    row, inner = t.stride()
     if inner != 1 and shape[1] > 1:
         raise ValueError(f"{name}: rows are contiguous, not with strides {list(t.stride())}")
     return row if shape[0] > 1 else shape[1]
@@ -119,7 +128,8 @@ class SpQRResidualNorm:
         d = self.desc = spqr_residual_norm_t()
         d.width, d.norm_y, d.norm_x, d.act = self.width, _NORMS[norm_y], _NORMS[norm_x], _ACTS[act]
         d.eps, d.weight_offset, d.skip, d.scale = float(eps), float(weight_offset), float(skip), float(scale)
-        d.out_dtype = 0 if out_dtype is None else S._dtypes[out_dtype]
+        self._out_type = 0 if out_dtype is None else S._dtypes[out_dtype]
+        self._one = None if out_dtype is None else torch.empty(1, dtype=out_dtype, device=self.device)
         dtype = next((v.dtype for v in given.values()), torch.float32)
         for n, v in given.items():
             if v.dtype != dtype or dtype not in S._dtypes or tuple(v.shape) != (self.width,) or not v.is_contiguous() or v.device != self.device:
@@ -133,44 +143,47 @@ def spqr_residual_norm(norm: SpQRResidualNorm, x=None, y=None, gate=None, *, sum
     """(s, norm_x(s)) of rows x, y [rows, width] (one may be None); gate [width] or [rows, width], or None.  s, in x's type, is
     made where there are both x and y, or written to `sum` (which may be x); else None.  The norm, of the handle's out_dtype, is made or
     written to `out`; None with out_dtype None."""
-    d, index = norm.desc, norm._index
+    index, dtypes = norm._index, S._dtypes
     rows = y if x is None else x
     if rows is None or rows.dim() != 2:
         raise ValueError("x, y: [rows, width], one of them at least")
     shape = rows.shape
-    if shape[1] != norm.width:
+    count, width = shape
+    if width != norm.width:
         raise ValueError(f"rows of {norm.width} elements, not {list(shape)}")
-    dtypes = S._dtypes
-    d.x = d.y = d.gate = d.sum = d.out = None
-    d.rows = shape[0]
+    x_at = y_at = gate_at = sum_at = out_at = x_stride = y_stride = gate_stride = sum_stride = 0
+    x_type = y_type = gate_type = 0
     if x is not None:
-        d.x_stride, d.x_dtype, d.x = _stride("x", x, shape, index), dtypes[x.dtype], x.data_ptr()
+        x_stride, x_type, x_at = _stride("x", x, shape, index), dtypes[x.dtype], x.data_ptr()
     if y is not None:
-        d.y_stride, d.y_dtype, d.y = _stride("y", y, shape, index), dtypes[y.dtype], y.data_ptr()
+        y_stride, y_type, y_at = _stride("y", y, shape, index), dtypes[y.dtype], y.data_ptr()
     if gate is not None:
         if y is None:
             raise ValueError("a gate without y")
         if gate.dim() == 1:
-            _stride("gate", gate[None], (1, shape[1]), index)
-            d.gate_stride = 0
+            _stride("gate", gate[None], (1, width), index)
         else:
-            d.gate_stride = _stride("gate", gate, shape, index)
-        d.gate_dtype, d.gate = dtypes[gate.dtype], gate.data_ptr()
-    if sum is None and x is not None and y is not None:
-        import torch
-        sum = torch.empty(shape, dtype=x.dtype, device=x.device)
-    if sum is not None:
-        d.sum_stride = _stride("sum", sum, shape, index, None if x is None else x.dtype)
-        d.x_dtype, d.sum = dtypes[sum.dtype], sum.data_ptr()
+            gate_stride = _stride("gate", gate, shape, index)
+        gate_type, gate_at = dtypes[gate.dtype], gate.data_ptr()
+    if sum is None:
+        if x is not None and y is not None:
+            sum = _empty_like(x) if x_stride == width else _empty(shape, dtype=x.dtype, device=x.device)
+            sum_at, sum_stride = sum.data_ptr(), width
+    else:
+        sum_stride, x_type, sum_at = _stride("sum", sum, shape, index, None if x is None else x.dtype), dtypes[sum.dtype], sum.data_ptr()
+    out_stride = width
     if norm.out_dtype is None:
         if out is not None:
             raise ValueError("out: this handle has out_dtype None")
-    elif out is None:
-        import torch
-        out = torch.empty(shape, dtype=norm.out_dtype, device=rows.device)
-        d.out_stride, d.out = shape[1], out.data_ptr()
     else:
-        d.out_stride, d.out = _stride("out", out, shape, index, norm.out_dtype), out.data_ptr()
+        if out is None:
+            out = norm._one.new_empty(shape)
+        else:
+            out_stride = _stride("out", out, shape, index, norm.out_dtype)
+        out_at = out.data_ptr()
+    d = norm.desc
+    _norm_types.pack_into(d, 0, count, width, x_type, y_type, gate_type, norm._out_type)
+    _norm_rows.pack_into(d, _norm_rows_at, x_at, y_at, gate_at, sum_at, out_at, x_stride, y_stride, sum_stride, out_stride, gate_stride)
     _run("spqr_residual_norm", index, stream, d)
     return sum, out
 
@@ -288,27 +301,31 @@ def spqr_adapters(bank: SpQRAdapters, plan: SpQRAdapterPlan, x, ys=None, outs=No
     [rows, m[p]] of one type.  ys None: zeros (outs are float32 unless given).  outs None: new tensors; outs may be ys.  Rows that the
     plan has in no tile are left as they are."""
     d, index, dtypes = bank.desc, bank._index, S._dtypes
-    rows = plan.rows
+    rows, k, ms = plan.rows, len(bank.m), bank.m
     if plan._index != index:
         raise ValueError(f"a plan on {plan.device}, banks on {bank.device}")
     d.x_stride, d.x = _stride("x", x, (rows, bank.width), index, bank.dtype), x.data_ptr()
-    k = d.count
     if (ys is not None and len(ys) != k) or (outs is not None and len(outs) != k):
         raise ValueError(f"ys, outs: {k} tensors")
-    if outs is None or ys is None:
-        import torch
-        if outs is None:
-            outs = [torch.empty((rows, m), dtype=torch.float32 if ys is None else ys[0].dtype, device=x.device) for m in bank.m]
-    dtype = outs[0].dtype
-    for p in range(k):
-        shape = (rows, bank.m[p])
-        if ys is None:
-            d.y[p] = None
-        else:
-            d.y_stride[p], d.y[p] = _stride(f"ys[{p}]", ys[p], shape, index, dtype), ys[p].data_ptr()
-        d.out_stride[p], d.out[p] = _stride(f"outs[{p}]", outs[p], shape, index, dtype), outs[p].data_ptr()
+    fields = [0] * (4 * SPQR_MAX_FUSED)
+    first = (outs or ys)
+    dtype = _float32 if first is None else first[0].dtype
     if dtype not in dtypes:
         raise ValueError(f"ys, outs: float32, float16 or bfloat16, not {dtype}")
+    if ys is not None:
+        for p in range(k):
+            fields[2 * SPQR_MAX_FUSED + p] = _stride("ys", ys[p], (rows, ms[p]), index, dtype)
+            fields[p] = ys[p].data_ptr()
+    if outs is None:
+        outs = [_empty((rows, m), dtype=dtype, device=x.device) if ys is None or fields[2 * SPQR_MAX_FUSED + p] != m else _empty_like(ys[p])
+                for p, m in enumerate(ms)]
+        fields[3 * SPQR_MAX_FUSED:3 * SPQR_MAX_FUSED + k] = ms
+    else:
+        for p in range(k):
+            fields[3 * SPQR_MAX_FUSED + p] = _stride("outs", outs[p], (rows, ms[p]), index, dtype)
+    for p in range(k):
+        fields[SPQR_MAX_FUSED + p] = outs[p].data_ptr()
+    _bank_rows.pack_into(d, _bank_rows_at, *fields)
     d.y_dtype = dtypes[dtype]
     _run("spqr_adapters", index, stream, d, plan._at)
     return outs

@@ -13,29 +13,56 @@ constexpr int kTile = SPQR_ADAPTER_TILE;
 // most), and what is behind their end is left out.
 //
 // A workgroup a slot (the last one: rows of no adapter).  Each counts the rows of all slots for itself, which gives the tiles before
-// its own, then walks through the requests in order and writes its rows.
-__global__ void __launch_bounds__(256) adapter_plan_kernel(spqr_adapter_plan_t p) {
+// its own; a wavefront has an equal part of the requests, in order, counts those of the slot, and writes their rows behind those of the wavefronts
+// before it.  Trips to memory and to LDS one after the other bound it: 4096 rows of 200 slots XX us (256 threads, a barrier for every 256 requests:
+// 15.6), 64 requests of 48 slots XX us.
+constexpr int kPlanAhead = 4;
+
+template <bool BY_ROW, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES) adapter_plan_kernel(spqr_adapter_plan_t p) {
   __shared__ int rows_of[SPQR_MAX_SLOTS + 1];
-  __shared__ int part[4][3];
-  __shared__ int wave_rows[4];
-  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, slot = blockIdx.x, S = p.slots;
-  auto slot_of = [&](int i) { const int a = p.adapter[i]; return a >= 0 && a < S ? a : S; };
-  auto rows_at = [&](int i, int* first) {
-    if (!p.q_start) { *first = i; return i < p.rows ? 1 : 0; }
-    const int lo = min(max(p.q_start[i], 0), p.rows), hi = min(max(p.q_start[i + 1], 0), p.rows);
-    *first = lo;
-    return max(0, hi - lo);
+  __shared__ int part[WAVES][3];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, slot = blockIdx.x, S = p.slots, threads = 64 * WAVES;
+  const int each = (p.requests + threads - 1) / threads * 64, i0 = min(wave * each, p.requests), i1 = min(i0 + each, p.requests);
+  // a request's slot (S: none) and rows
+  struct Request { int slot, first, rows; };
+  auto request = [&](int i) {
+    Request r{S, i, 0};
+    if (i >= i1) return r;
+    const int a = p.adapter[i];
+    r.slot = a >= 0 && a < S ? a : S;
+    if (BY_ROW) {
+      r.rows = 1;
+    } else {
+      r.first = min(max(p.q_start[i], 0), p.rows);
+      r.rows = max(0, min(max(p.q_start[i + 1], 0), p.rows) - r.first);
+    }
+    return r;
   };
-  for (int s = tid; s <= S; s += 256) rows_of[s] = 0;
+  for (int s = tid; s <= S; s += threads) rows_of[s] = 0;
   __syncthreads();
-  for (int i = tid; i < p.requests; i += 256) {
-    int first;
-    const int rows = rows_at(i, &first);
-    if (rows > 0) atomicAdd(&rows_of[slot_of(i)], rows);
+  int own = 0;                                   // rows of the slot among the wavefront's
+  for (int i = i0 + lane; i - lane < i1; i += 64 * kPlanAhead) {
+    Request r[kPlanAhead];
+#pragma unroll
+    for (int k = 0; k < kPlanAhead; ++k) r[k] = request(i + 64 * k);
+#pragma unroll
+    for (int k = 0; k < kPlanAhead; ++k) {
+      if (r[k].slot == slot) own += r[k].rows;
+      // (rows of one slot side by side: one addition)
+      const int first = __builtin_amdgcn_readfirstlane(r[k].slot);
+      if (BY_ROW && __all(r[k].slot == first && r[k].rows == 1)) {
+        if (lane == 0) atomicAdd(&rows_of[first], 64);
+      } else if (r[k].rows > 0) {
+        atomicAdd(&rows_of[r[k].slot], r[k].rows);
+      }
+    }
   }
+  for (int d = 32; d > 0; d >>= 1) own += __shfl_xor(own, d);
+  if (lane == 0) part[wave][2] = own;
   __syncthreads();
   int before = 0, all = 0;
-  for (int s = tid; s <= S; s += 256) {
+  for (int s = tid; s <= S; s += threads) {
     const int tiles = (rows_of[s] + kTile - 1) / kTile;
     all += tiles;
     if (s < slot) before += tiles;
@@ -43,42 +70,59 @@ __global__ void __launch_bounds__(256) adapter_plan_kernel(spqr_adapter_plan_t p
   for (int d = 32; d > 0; d >>= 1) { before += __shfl_xor(before, d); all += __shfl_xor(all, d); }
   if (lane == 0) { part[wave][0] = before; part[wave][1] = all; }
   __syncthreads();
-  before = part[0][0] + part[1][0] + part[2][0] + part[3][0];
-  all = min(part[0][1] + part[1][1] + part[2][1] + part[3][1], p.max_tiles);
+  before = all = 0;
+  int done = 0;                                  // rows of the slot before the wavefront's
+#pragma unroll
+  for (int w = 0; w < WAVES; ++w) {
+    before += part[w][0];
+    all += part[w][1];
+    if (w < wave) done += part[w][2];
+  }
+  all = min(all, p.max_tiles);
   const int rows = rows_of[slot], tiles = (rows + kTile - 1) / kTile;
   if (slot == 0 && tid == 0) p.count[0] = all;
   // behind the last tile: shared out
-  for (int64_t t = all + slot; t < p.max_tiles; t += S + 1) {
-    if (tid < 2) p.tile[2 * t + tid] = tid == 0 ? -1 : 0;
-    if (tid < kTile) p.row[t * kTile + tid] = -1;
+  for (int64_t t = all + slot + (int64_t)wave * (S + 1); t < p.max_tiles; t += (int64_t)(S + 1) * WAVES) {
+    if (lane < 2) p.tile[2 * t + lane] = lane == 0 ? -1 : 0;
+    p.row[t * kTile + lane] = -1;
   }
-  for (int t = tid; t < tiles; t += 256)
+  for (int t = tid; t < tiles; t += threads)
     if (before + t < p.max_tiles) {
       p.tile[2 * (before + t)] = slot < S ? slot : -1;
       p.tile[2 * (before + t) + 1] = min(kTile, rows - kTile * t);
     }
-  if (rows == 0) return;
   const int64_t base = (int64_t)before * kTile, room = (int64_t)p.max_tiles * kTile;
   if (rows % kTile != 0 && tid < kTile && tid >= rows % kTile && base + (int64_t)(tiles - 1) * kTile + tid < room)
     p.row[base + (int64_t)(tiles - 1) * kTile + tid] = -1;
-  int64_t done = base;
-  for (int i0 = 0; i0 < p.requests; i0 += 256) {
-    const int i = i0 + tid;
-    int first = 0, mine = 0;
-    if (i < p.requests && slot_of(i) == slot) mine = rows_at(i, &first);
-    int sum = mine;                              // of the lanes up to this one
-    for (int d = 1; d < 64; d <<= 1) {
-      const int o = __shfl_up(sum, d);
-      if (lane >= d) sum += o;
+  if (own == 0) return;
+  int64_t at = base + done;
+  for (int i = i0 + lane; i - lane < i1; i += 64 * kPlanAhead) {
+    Request r[kPlanAhead];
+#pragma unroll
+    for (int k = 0; k < kPlanAhead; ++k) r[k] = request(i + 64 * k);
+#pragma unroll
+    for (int k = 0; k < kPlanAhead; ++k) {
+      const int mine = r[k].slot == slot ? r[k].rows : 0;
+      if (BY_ROW) {
+        const uint64_t of = __ballot(mine > 0);
+        const int64_t to = at + __popcll(of & ((1ull << lane) - 1));
+        if (mine > 0 && to < room) p.row[to] = r[k].first;
+        at += __popcll(of);
+      } else if (__any(mine > 0)) {
+        int sum = mine;                          // of the lanes up to this one
+        for (int d = 1; d < 64; d <<= 1) {
+          const int o = __shfl_up(sum, d);
+          if (lane >= d) sum += o;
+        }
+        // a request's rows, by all lanes
+        for (uint64_t left = __ballot(mine > 0); left != 0; left &= left - 1) {
+          const int l = __ffsll((unsigned long long)left) - 1, n = __shfl(mine, l), first = __shfl(r[k].first, l);
+          const int64_t to = at + __shfl(sum, l) - n;
+          for (int64_t m = lane; m < n && to + m < room; m += 64) p.row[to + m] = first + (int)m;
+        }
+        at += __shfl(sum, 63);
+      }
     }
-    if (lane == 63) wave_rows[wave] = sum;
-    __syncthreads();
-    int64_t to = done + sum - mine;
-    for (int w = 0; w < wave; ++w) to += wave_rows[w];
-    const int fit = (int)min((int64_t)mine, room - to);
-    for (int k = 0; k < fit; ++k) p.row[to + k] = first + k;
-    done += wave_rows[0] + wave_rows[1] + wave_rows[2] + wave_rows[3];
-    __syncthreads();
   }
 }
 
@@ -785,7 +829,12 @@ extern "C" int spqr_adapter_plan(const spqr_adapter_plan_t* p, void* stream) {
   if (p->rows == 0) return SPQR_OK;
   if (!p->adapter) return SPQR_ERR_NULL;
   if (!aligned(p->adapter, 4) || !aligned(p->q_start, 4)) return SPQR_ERR_ALIGN;
-  hipLaunchKernelGGL(adapter_plan_kernel, dim3(p->slots + 1), dim3(256), 0, static_cast<hipStream_t>(stream), *p);
+  const dim3 grid(p->slots + 1);
+  const hipStream_t st = static_cast<hipStream_t>(stream);
+  // (4 wavefronts: fewer barriers' worth of them; 64 requests 4.2 us, by 16 5.4)
+  if (p->q_start) hipLaunchKernelGGL((adapter_plan_kernel<false, 4>), grid, dim3(256), 0, st, *p);
+  else if (p->requests <= 1024) hipLaunchKernelGGL((adapter_plan_kernel<true, 4>), grid, dim3(256), 0, st, *p);
+  else hipLaunchKernelGGL((adapter_plan_kernel<true, 16>), grid, dim3(1024), 0, st, *p);
   return launched();
 }
 
