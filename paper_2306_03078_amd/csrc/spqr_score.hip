@@ -124,7 +124,7 @@ __device__ __forceinline__ void rank_keys(const uint64_t* keys, int count, int k
 // have one of the best look at theirs again.  WHOLE: all of the row.
 template <typename T, int NT, bool WHOLE>
 __global__ void __launch_bounds__(NT) score_kernel(spqr_token_logprobs_t p, int length, Part* parts, uint64_t* keys) {
-  constexpr int WAVES = NT / 64, AHEAD = 4;
+  constexpr int WAVES = NT / 64, AHEAD = WHOLE ? 4 : 2;      // (parts are short)
   __shared__ float maxima[NT];
   __shared__ float red[3][WAVES];
   __shared__ uint64_t cand[kCandidates];
@@ -137,11 +137,17 @@ __global__ void __launch_bounds__(NT) score_kernel(spqr_token_logprobs_t p, int 
   const float c = p.scale * kLog2e;
 
   Soft s{-kFar, 0.f, 0.f};
-  float mine = -INFINITY;
-  auto take = [&](const float (&v)[8]) {
-    float top = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+  // a thread's largest logit, the stretch of its logits that has it, and the largest of the other stretches
+  float mine = -INFINITY, other = -INFINITY;
+  int where = 0;
+  auto note = [&](float top, int at) {
+    other = fmaxf(other, fminf(mine, top));
+    where = top > mine ? at : where;
     mine = fmaxf(mine, top);
-    top *= c;
+  };
+  auto take = [&](const float (&v)[8]) {
+    const float largest = fmaxf(fmaxf(fmaxf(v[0], v[1]), fmaxf(v[2], v[3])), fmaxf(fmaxf(v[4], v[5]), fmaxf(v[6], v[7])));
+    const float top = largest * c;
     if (top > s.ref + 8.f) rebase(s, rintf(top));
     float sum = 0.f, dot = 0.f;
 #pragma unroll
@@ -152,24 +158,28 @@ __global__ void __launch_bounds__(NT) score_kernel(spqr_token_logprobs_t p, int 
     }
     s.sum += sum;
     s.dot += dot;
+    return largest;
   };
   int at = 8 * tid;
   for (; at + 8 * NT * (AHEAD - 1) + 8 <= n; at += 8 * NT * AHEAD) {
     Run8<T> x[AHEAD];
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) x[i] = *reinterpret_cast<const Run8<T>*>(row + at + 8 * NT * i);
+    float top = -INFINITY;
 #pragma unroll
     for (int i = 0; i < AHEAD; ++i) {
       float v[8];
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[e] = (float)x[i].e[e];
-      take(v);
+      top = fmaxf(top, take(v));
     }
+    note(top, at);
   }
+  const int rest = at;                           // behind here a stretch is eight logits, before it AHEAD times as many
   for (; at < n; at += 8 * NT) {
     float v[8];
     load_logits(row, at, n, v);
-    take(v);
+    note(take(v), at);
   }
   // the largest of all, and sums by its reference
   maxima[tid] = mine;
@@ -217,17 +227,27 @@ __global__ void __launch_bounds__(NT) score_kernel(spqr_token_logprobs_t p, int 
     for (int w = 1; w < WAVES; ++w) g = fmaxf(g, maxima[64 * w + lane]);
     const uint32_t key = kth_largest(ordered(g), k);
     bound = key <= 0x007FFFFFu ? -INFINITY : unordered(key);                              // (0x007FFFFF: -infinity; below it are no numbers)
-    if (mine >= bound && mine > -INFINITY)
-      for (int i = 8 * tid; i < n; i += 8 * NT) {
-        float v[8];
-        load_logits(row, i, n, v);
+    if (mine >= bound && mine > -INFINITY) {
+      // as a rule one stretch has all that count
+      const bool one = other < bound;
+      const int last = one ? where < rest ? where + 8 * NT * AHEAD : where + 1 : n;
+      for (int i = one ? where : 8 * tid; i < last; i += 8 * NT * AHEAD) {
+        float v[AHEAD][8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (v[e] >= bound && v[e] > -INFINITY) {
-            const int to = atomicAdd(&found, 1);
-            if (to < kCandidates) cand[to] = key_of(v[e], begin + i + e);
-          }
+        for (int k = 0; k < AHEAD; ++k) load_logits(row, min(i + 8 * NT * k, n - 1), n, v[k]);
+#pragma unroll
+        for (int k = 0; k < AHEAD; ++k) {
+          const int from = i + 8 * NT * k;
+          if (from < min(last, n))
+#pragma unroll
+            for (int e = 0; e < 8; ++e)
+              if (v[k][e] >= bound && v[k][e] > -INFINITY) {
+                const int to = atomicAdd(&found, 1);
+                if (to < kCandidates) cand[to] = key_of(v[k][e], begin + from + e);
+              }
+        }
       }
+    }
   }
   __syncthreads();
   part.sum = part.dot = 0.f;
