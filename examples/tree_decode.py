@@ -4,13 +4,17 @@ that one pass verifies; both give the same tokens.
 A step of either kind is, on one stream and without a copy to the host before its logits:
 
     spqr_cache_plan                        pages, slots, positions, masks of the new tokens
+    spqr_adapter_plan                      the step's rows by their sequences' adapters
     per layer: spqr_gemm_fused             q, k, v
+               spqr_adapters               ... and what a sequence's adapter adds to them
                spqr_cache_store            rotary embedding, keys and values to the cache
                spqr_tree_attention
                spqr_gemm_smallbatch, ...   o, gate and up, down
+               spqr_residual_norm          norms, gates and sums between them
+    spqr_token_logprobs                    the choice behind every new token, and how probable it is
     spqr_cache_keep                        the accepted path's rows move together, the lengths grow
 
-Weights are random.  The drafter guesses from the sequences that token-by-token decoding gave (right with a given probability a
+Weights are random; every second sequence has one of two adapters.  The drafter guesses from the sequences that token-by-token decoding gave (right with a given probability a
 token, wrong siblings beside it): it stands for a small model.
 
     python examples/tree_decode.py
@@ -26,6 +30,7 @@ import torch
 
 sys.path.insert(0, os.path.dirname(os.path.dirname(os.path.abspath(__file__))))
 import paper_2306_03078_amd as P  # noqa: E402
+import paper_2306_03078_amd.block_binding as K  # noqa: E402
 import paper_2306_03078_amd.serve_binding as S  # noqa: E402
 import spqr_synth as synth  # noqa: E402
 
@@ -45,6 +50,16 @@ class Decoder:
         kv = kv_heads * self.D
         self.blocks = [dict(qkv=[matrix(hidden, hidden, i, 0), matrix(kv, hidden, i, 1), matrix(kv, hidden, i, 2)], o=matrix(hidden, hidden, i, 3),
                             gate_up=[matrix(ffn, hidden, i, 4), matrix(ffn, hidden, i, 5)], down=matrix(hidden, ffn, i, 6)) for i in range(layers)]
+        # two adapters of 16 ranks (the second of 5) beside q, k and v of each layer
+        down = lambda: torch.randn(2, 16, hidden, device="cuda:0", generator=g).mul_(hidden ** -0.5).half()  # noqa: E731
+        up = lambda m: torch.randn(2, m, 16, device="cuda:0", generator=g).half()  # noqa: E731
+        self.ranks = torch.tensor([16, 5], dtype=torch.int32, device="cuda:0")
+        self.adapters = [([down() for _ in range(3)], [up(m) for m in (hidden, kv, kv)]) for _ in range(layers)]
+        # x; x + norm(y), both before the next block; norm(y); silu(g) * norm(y); and what the head takes
+        norm = K.SpQRResidualNorm
+        self.before, self.join = norm(hidden), norm(hidden, norm_y="rms")
+        self.q_norm, self.k_norm, self.gate_norm = (norm(n, norm_y="rms", norm_x=None, out_dtype="float32") for n in (hidden, kv, ffn))
+        self.gated, self.last = norm(ffn, norm_y="rms", norm_x=None, act="silu"), norm(hidden, norm_y="rms", out_dtype="float32")
         angle = torch.arange(positions, dtype=torch.float64)[:, None] * 10000.0 ** (-torch.arange(0, self.D, 2, dtype=torch.float64) / self.D)
         self.rotary = torch.cat([angle.cos(), angle.sin()], 1).float().cuda()
 
@@ -55,21 +70,28 @@ class Decoder:
         return S.SpQRStep(k, v, self.heads, requests=requests, tokens=tokens, max_pages=width, mask_words=-(-max_fresh // 64), max_fresh=max_fresh,
                           rotary=self.rotary, parent=torch.full((tokens,), -1, dtype=torch.int32, device="cuda:0"))
 
-    @staticmethod
-    def norm(x):
-        return x * torch.rsqrt(x.square().mean(1, keepdim=True) + 1e-6)
+    def banks(self, rows):
+        """The layers' adapters for steps of up to `rows` rows; one scratch for all."""
+        banks = []
+        for A, B in self.adapters:
+            banks.append(K.SpQRAdapters(A, B, rank=self.ranks, rows=rows, workspace=banks[0].workspace if banks else None))
+        return banks
 
-    def logits(self, step, tokens):
+    def logits(self, step, tokens, banks, plan):
         """The planned step's rows: tokens [rows] -> [rows, vocab].  (Rows that belong to no sequence give anything.)"""
+        norm = K.spqr_residual_norm
         x = self.embedding[tokens]
+        _, h = norm(self.before, x)
         for i, block in enumerate(self.blocks):
-            q, k, v = P.spqr_gemm_fused(block["qkv"], self.norm(x).half())
-            q = S.spqr_cache_store(step, self.norm(q), self.norm(k), v / self.hidden ** 0.5, layer=i)
+            q, k, v = P.spqr_gemm_fused(block["qkv"], h)
+            K.spqr_adapters(banks[i], plan, h, [q, k, v], outs=[q, k, v])
+            q = S.spqr_cache_store(step, norm(self.q_norm, y=q)[1], norm(self.k_norm, y=k)[1], v / self.hidden ** 0.5, layer=i)
             a = S.spqr_tree_attention(step, q, layer=i, out=torch.zeros_like(q))
-            x = x + self.norm(P.spqr_gemm_smallbatch(block["o"], a.view(len(tokens), -1)))
-            gate, up = P.spqr_gemm_fused(block["gate_up"], self.norm(x).half())
-            x = x + self.norm(P.spqr_gemm_smallbatch(block["down"], (torch.nn.functional.silu(self.norm(gate)) * self.norm(up)).half()))
-        return self.norm(x) @ self.head.T
+            x, h = norm(self.join, x, P.spqr_gemm_smallbatch(block["o"], a.view(len(tokens), -1)))
+            gate, up = P.spqr_gemm_fused(block["gate_up"], h)
+            _, h = norm(self.gated, y=up, gate=norm(self.gate_norm, y=gate)[1])
+            x, h = norm(self.join if i + 1 < self.layers else self.last, x, P.spqr_gemm_smallbatch(block["down"], h))
+        return h @ self.head.T
 
 
 class Session:
@@ -77,6 +99,9 @@ class Session:
 
     def __init__(self, model, requests, tokens, length, max_fresh):
         self.model, self.step = model, model.step(requests, tokens, length, max_fresh)
+        self.banks, self.plan = model.banks(tokens), K.SpQRAdapterPlan(tokens, 2)
+        self.adapter = torch.tensor([r // 2 % 2 if r % 2 == 0 else -1 for r in range(requests)], dtype=torch.int32, device="cuda:0")
+        self.scores = K.SpQRScores(tokens, model.embedding.shape[0], given=0, top=1)
 
     def verify(self, ids, parents):
         """Greedy choice behind every new token, as lists per sequence; the step stays open until keep()."""
@@ -86,8 +111,9 @@ class Session:
         step.fresh.copy_(torch.tensor([len(x) for x in ids], dtype=torch.int32))
         step.parent.copy_(torch.tensor(tree + [-1] * pad, dtype=torch.int32))
         S.spqr_cache_plan(step)
-        self.best = self.model.logits(step, torch.tensor(flat + [0] * pad, device="cuda:0"))
-        choice = self.best.argmax(1).tolist()
+        K.spqr_adapter_plan(self.plan, self.adapter, step.q_start)
+        self.best = self.model.logits(step, torch.tensor(flat + [0] * pad, device="cuda:0"), self.banks, self.plan)
+        choice = K.spqr_token_logprobs(self.scores, self.best).top_token[:, 0].tolist()
         if int(step.ends_out[2]):
             raise RuntimeError(f"the cache lacks {int(step.ends_out[2])} pages")
         starts = np.cumsum([0] + [len(x) for x in ids])
