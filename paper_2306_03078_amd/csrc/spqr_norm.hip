@@ -3,7 +3,23 @@
 
 namespace spqr_blk {
 
-using spqr::wave_allreduce;
+// Adds what a data-parallel move brings (0 where it brings nothing).
+template <int CTRL, int ROWS>
+__device__ __forceinline__ float plus(float v) {
+  return v + __uint_as_float(__builtin_amdgcn_update_dpp(0, __float_as_uint(v), CTRL, ROWS, 0xF, false));
+}
+// Sum over 16 lanes, in the last of them; over the wavefront, the same in all of its lanes.
+__device__ __forceinline__ float sum16(float v) {
+  v = plus<0x111, 0xF>(v);                       // row_shr:1, 2, 4, 8
+  v = plus<0x112, 0xF>(v);
+  v = plus<0x114, 0xF>(v);
+  return plus<0x118, 0xF>(v);
+}
+__device__ __forceinline__ float lane_of(float v, int lane) { return __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(v), lane)); }
+__device__ __forceinline__ float sum64(float v) {
+  v = plus<0x142, 0xA>(sum16(v));                // row_bcast:15, then :31: a row's sum to the next one, the first half's to the second
+  return lane_of(plus<0x143, 0xC>(v), 63);
+}
 
 // Sum over the `lanes` threads of a row (a power of two; whole wavefronts above 64), in every one of them.  part: two buffers of one float a
 // wavefront, taken in turn, so that one barrier a sum is enough (the next sum's stands between its readers and the next writers).
@@ -11,27 +27,17 @@ struct RowSum {
   float (*part)[16];
   int lanes, turn;
   __device__ __forceinline__ float operator()(float v) {
-    const int lane = threadIdx.x & 63;
     if (lanes < 64) {
       for (int d = lanes >> 1; d > 0; d >>= 1) v += __shfl_xor(v, d);
       return v;
     }
-    v = wave_allreduce(v, lane);
+    v = sum64(v);
     if (lanes > 64) {
-      const int wave = threadIdx.x >> 6, waves = lanes >> 6, first = wave & ~(waves - 1);
+      const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), waves = lanes >> 6;
       if (lane == 0) part[turn][wave] = v;
       __syncthreads();
-      if (waves == 2) {
-        v = part[turn][first] + part[turn][first + 1];
-      } else {
-        v = 0.f;
-#pragma unroll
-        for (int w = 0; w < 16; w += 4)          // (all are asked for at once)
-          if (w < waves) {
-            const float4 f = *reinterpret_cast<const float4*>(&part[turn][first + w]);
-            v += (f.x + f.y) + (f.z + f.w);
-          }
-      }
+      // 16 lanes take the row's wavefronts
+      v = lane_of(sum16((lane & 15) < waves ? part[turn][(wave & ~(waves - 1)) + (lane & 15)] : 0.f), 15);
       turn ^= 1;
     }
     return v;
@@ -124,7 +130,7 @@ __device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Pla
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] -= mean;
   }
-  const float r = 1.f / sqrtf(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
+  const float r = __builtin_amdgcn_rsqf(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     float x[8], y[8];
@@ -151,8 +157,9 @@ template <typename T> struct TypeOf { static constexpr int value = SPQR_F32; };
 template <> struct TypeOf<_Float16> { static constexpr int value = SPQR_F16; };
 template <> struct TypeOf<__bf16> { static constexpr int value = SPQR_BF16; };
 
-// `lanes` threads a row, rows in turn; the next row's terms are on their way while one is worked out.
-template <typename X, typename Y, bool ODD, int CH>
+// `lanes` threads a row.  MANY: rows in turn; the next row's terms are on their way while one is worked out (4096 gated rows of 6656: 119 us with a
+// workgroup a row).
+template <typename X, typename Y, bool ODD, bool MANY, int CH = 1>
 __global__ void __launch_bounds__(1024 / CH) norm_rows_kernel(spqr_residual_norm_t p, int lanes) {
   __shared__ __align__(16) float part[2][16];
   constexpr int XT = TypeOf<X>::value, YT = TypeOf<Y>::value;
@@ -198,7 +205,7 @@ __global__ void __launch_bounds__(1024 / CH) norm_rows_kernel(spqr_residual_norm
       if (has_gate) floats_at<ODD>(g[c], p.gate_dtype, at[c], f[c]);
     }
     const int64_t next = first + (int64_t)gridDim.x * per;
-    if (next < p.rows) {
+    if (MANY && next < p.rows) {
       t = min(next + mine, (int64_t)p.rows - 1);
       load_row(t, has_gate && p.gate_stride != 0);
     }
@@ -207,9 +214,13 @@ __global__ void __launch_bounds__(1024 / CH) norm_rows_kernel(spqr_residual_norm
 #pragma unroll
       for (int c = 0; c < CH; ++c) {
         if (has_gate) {
-          if (p.act != SPQR_ACT_NONE)
+          if (p.act == SPQR_ACT_SIGMOID) {
+#pragma unroll
+            for (int e = 0; e < 8; ++e) f[c][e] = activated(SPQR_ACT_SIGMOID, f[c][e]);
+          } else if (p.act != SPQR_ACT_NONE) {
 #pragma unroll
             for (int e = 0; e < 8; ++e) f[c][e] = activated(p.act, f[c][e]);
+          }
 #pragma unroll
           for (int e = 0; e < 8; ++e) v[c][e] *= f[c][e];
         }
@@ -231,6 +242,7 @@ __global__ void __launch_bounds__(1024 / CH) norm_rows_kernel(spqr_residual_norm
       for (int c = 0; c < CH; ++c)
         if (live && at[c].count > 0) store_row8_as(p.out_dtype, p.out, here * p.out_stride, at[c].col, n, v[c]);
     }
+    if (!MANY) return;
   }
 }
 
@@ -239,8 +251,8 @@ constexpr int64_t kThreads = 512 * 1024;         // as many as run at once
 template <typename X, typename Y, bool ODD>
 static void launch_rows(const spqr_residual_norm_t& p, int lanes, int threads, int64_t groups, hipStream_t st) {
   const int64_t most = kThreads / threads;
-  const dim3 grid((unsigned)(groups < most ? groups : most));
-  hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, 1>), grid, dim3(threads), 0, st, p, lanes);
+  if (groups <= most) hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, false>), dim3((unsigned)groups), dim3(threads), 0, st, p, lanes);
+  else hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, true>), dim3((unsigned)most), dim3(threads), 0, st, p, lanes);
 }
 
 template <typename X, bool ODD>
