@@ -634,10 +634,19 @@ __device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, 
     if (CHUNKS == 1 && NS < 4) step(next_w, w, 1, m_of(i + 1), m_of(i + 2));
     else step(w, next_w, 1, m_of(i + 1), m_of(i + 2));
   }
+  // Fewer than 64 m: every element of y is asked for by itself, all of 16 rows at once, those behind the end and of no row too (the last there are).
   const int end = first + 256 * steps;
   if (end < m1)
     for (int s = 0; s < NS; ++s) {
       f32x4 acc[4];
+      Y ends[4][4];
+      int64_t r[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        r[i] = __shfl(t.row, 16 * (sub0 + s) + 4 * g + i);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) ends[i][j] = y[max(r[i], (int64_t)0) * y_stride + (has_y ? min(end + j, m1 - 1 - 4 * l16) : 0)];
+      }
       zero(acc);
 #pragma unroll
       for (int k = 0; k < CHUNKS; ++k) {
@@ -645,13 +654,11 @@ __device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, 
         multiply(acc, w, s, k);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const int r = __shfl(t.row, 16 * (sub0 + s) + 4 * g + i);
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
         for (int j = 0; j < 4; ++j)
-          if (end + 4 * l16 + j < m1 && r >= 0)
-            out[r * out_stride + end + j] = (Y)fmaf(factors[16 * s + 4 * g + i], acc[j][i], has_y ? (float)y[r * y_stride + end + j] : 0.f);
-      }
+          if (end + 4 * l16 + j < m1 && r[i] >= 0)
+            out[r[i] * out_stride + end + j] = (Y)fmaf(factors[16 * s + 4 * g + i], acc[j][i], has_y ? (float)ends[i][j] : 0.f);
     }
 }
 
@@ -703,12 +710,14 @@ __global__ void __launch_bounds__(256, KIND == kLong ? 1 : KIND == kAny ? 2 : 3)
   __shared__ f32x4 sums[16 * 64];
   __shared__ x8<T> vs[N * 8 * 64];               // 64 rows of 64 ranks, or 16 of 256
   __shared__ float factors[kTile];
-  const unsigned pieces = min(uniform(c.count), c.max_tiles) * c.pieces, each = pieces / gridDim.x, more = pieces % gridDim.x;
+  // (Ranks above 64 take 16 rows at a time: where pieces are few, 64 rows are four of them.)
+  const unsigned all = min(uniform(c.count), c.max_tiles) * c.pieces, parts = LONG && all * 4 <= gridDim.x ? 4 : 1;
+  const unsigned pieces = all * parts, each = pieces / gridDim.x, more = pieces % gridDim.x;
   unsigned at = each * blockIdx.x + min(blockIdx.x, more);
   const unsigned end = at + each + (blockIdx.x < more);
   while (at < end) {
     int piece = (int)(at % c.pieces), which = 0;
-    const int tile = (int)(at / c.pieces);
+    const int tile = (int)(at / c.pieces / parts), part = (int)(at / c.pieces % parts);
     for (; piece >= (c.p[which].m + 255) / 256; ++which) piece -= (c.p[which].m + 255) / 256;
     const Projection& p = c.p[which];
     const int run = (int)min(end - at, (unsigned)((p.m + 255) / 256 - piece)), m0 = 256 * piece, m1 = min(p.m, m0 + 256 * run);
@@ -716,6 +725,7 @@ __global__ void __launch_bounds__(256, KIND == kLong ? 1 : KIND == kAny ? 2 : 3)
     const Tile t = tile_at(c, tile);
     if (t.rows == 0) continue;
     const int rank = rank_of(p, t.slot);
+    if (part > 0 && (rank <= 64 || 16 * part >= t.rows)) continue;
     if (rank <= 0) {
       copy_rows<Y>(p, t, m0, m1);
       continue;
@@ -724,8 +734,8 @@ __global__ void __launch_bounds__(256, KIND == kLong ? 1 : KIND == kAny ? 2 : 3)
 #define SPQR_EXPAND(H, NS, SUB) expand_rows<T, Y, H, NS>(c, p, t, tile, SUB, rank, m0, m1, sums, vs, factors)
 #define SPQR_EXPAND_ROWS(H) do { if (KIND == kFew || t.rows <= 16) SPQR_EXPAND(H, 1, 0); else if (t.rows <= 32) SPQR_EXPAND(H, 2, 0); else SPQR_EXPAND(H, 4, 0); } while (0)
     if (LONG && rank > 64) {
-      for (int sub = 0; 16 * sub < t.rows; ++sub) {
-        if (sub > 0) __syncthreads();
+      for (int sub = part; 16 * sub < t.rows; sub += LONG && parts > 1 ? 4 : 1) {
+        if (sub > part) __syncthreads();
         if (rank <= 128) SPQR_EXPAND(LONG ? 4 : 2, 1, sub);
         else SPQR_EXPAND(LONG ? 8 : 2, 1, sub);
       }
@@ -776,7 +786,7 @@ static Call call_of(const spqr_adapters_t* a, const spqr_adapter_plan_t* plan, i
 template <typename T, typename Y>
 static void launch_expand(const Call& c, bool longer, int pieces, hipStream_t st) {
   // as many workgroups as the card's registers have room for
-  if (longer) hipLaunchKernelGGL((expand_kernel<T, Y, kLong>), dim3(min(pieces, 256)), dim3(256), 0, st, c);
+  if (longer) hipLaunchKernelGGL((expand_kernel<T, Y, kLong>), dim3(min(pieces, 64) * 4), dim3(256), 0, st, c);
   else if (c.rows <= 16) hipLaunchKernelGGL((expand_kernel<T, Y, kFew>), dim3(min(pieces, 768)), dim3(256), 0, st, c);
   else hipLaunchKernelGGL((expand_kernel<T, Y, kAny>), dim3(min(pieces, 512)), dim3(256), 0, st, c);
 }
