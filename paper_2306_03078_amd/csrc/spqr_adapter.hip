@@ -255,7 +255,6 @@ struct Call {
   Cut cut;
   int width, slots, rows, max_tiles, v_tiles;
   int pieces;                                    // of 256 elements, of a row of all outputs
-  int rank_tile[SPQR_MAX_FUSED * SPQR_MAX_RANK / 16];      // projection + 256 * its tile of 16 ranks
 };
 __device__ __forceinline__ float* v_of(const Call& c, int split, int tile, int half, int sub) {
   return c.v + (((int64_t)split * c.v_tiles + tile) * c.cut.rank_halves + half) * (4 * 512) + sub * 512;
@@ -328,9 +327,10 @@ __device__ __forceinline__ void shrink_few(const Call& c, const Tile& t, const P
 }
 
 // More rows: NS * 16 of them through LDS, a stage at a time (rows of 256 bytes, 16-byte pieces turned by the row so that 16 rows' are in all banks);
-// each wavefront has NR tiles of 16 ranks of its own, of any projections.
+// each wavefront has NR tiles of 16 ranks of its own, of any projections, of those that the slot's ranks fill
+// (all that the bank has room for, in four where three would do: 39 us in place of 35 for 5000 rows of three projections, ranks of 8 to 64).
 template <typename T, int NR, int NS>
-__device__ __forceinline__ void shrink_many(const Call& c, const Tile& t, int first, int split, int s0, int s1, x8<T>* xs) {
+__device__ __forceinline__ void shrink_many(const Call& c, const Tile& t, const int (&tiles_of)[SPQR_MAX_FUSED], int first, int end, int split, int s0, int s1, x8<T>* xs) {
   const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), l16 = lane & 15, g = lane >> 4, n = c.width;
   const int steps = (n + 127) / 128 * 4;
   // a thread's piece of NS rows
@@ -340,13 +340,16 @@ __device__ __forceinline__ void shrink_many(const Call& c, const Tile& t, int fi
   for (int i = 0; i < NS; ++i) x[i] = static_cast<const T*>(c.x) + max(__shfl(t.row, 16 * i + row0), 0) * c.x_stride + 8 * piece;
   // a wavefront's tiles; one that is none reads those of the first
   const x8<T>* A[NR];
-  bool there[NR];
+  int of[NR], tile[NR];
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
-    const int i = first + wave + 4 * r, of = c.rank_tile[i < c.cut.rank_tiles ? i : first];
-    const Projection& p = c.p[of & 255];
-    there[r] = i < c.cut.rank_tiles && 16 * (of >> 8) < rank_of(p, t.slot);
-    A[r] = slot_of<T>(c, p, t.slot) + (int64_t)(of >> 8) * steps * 64 + lane;
+    const int i = first + wave + 4 * r;
+    of[r] = 0;
+    tile[r] = i < end ? i : first;
+#pragma unroll
+    for (int p = 0; p < SPQR_MAX_FUSED - 1; ++p)
+      if (of[r] == p && tile[r] >= tiles_of[p]) { tile[r] -= tiles_of[p]; ++of[r]; }
+    A[r] = slot_of<T>(c, c.p[of[r]], t.slot) + (int64_t)tile[r] * steps * 64 + lane;
   }
   f32x4 acc[NR][NS];
 #pragma unroll
@@ -388,10 +391,9 @@ __device__ __forceinline__ void shrink_many(const Call& c, const Tile& t, int fi
   }
 #pragma unroll
   for (int r = 0; r < NR; ++r)
-    if (there[r]) {
-      const int of = c.rank_tile[first + wave + 4 * r];
+    if (first + wave + 4 * r < end) {
 #pragma unroll
-      for (int i = 0; i < NS; ++i) put(c, c.p[of & 255], split, blockIdx.y, of >> 8, i, lane, acc[r][i]);
+      for (int i = 0; i < NS; ++i) put(c, c.p[of[r]], split, blockIdx.y, tile[r], i, lane, acc[r][i]);
     }
 }
 
@@ -415,11 +417,18 @@ __global__ void __launch_bounds__(256) shrink_kernel(Call c) {
     else shrink_few<T, 4>(c, t, c.p[p], kWaveTiles * z, tiles, split, s0, s1, red);
     return;
   }
-  const int first = 4 * kWaveTiles * (int)blockIdx.z, left = c.cut.rank_tiles - first;
+  int tiles_of[SPQR_MAX_FUSED], end = 0;
+#pragma unroll
+  for (int p = 0; p < SPQR_MAX_FUSED; ++p) {
+    tiles_of[p] = (rank_of(c.p[p], t.slot) + 15) / 16;
+    end += tiles_of[p];
+  }
+  const int first = 4 * kWaveTiles * (int)blockIdx.z, left = end - first;
   if (left <= 0) return;
-#define SPQR_SHRINK(NR) do { if (t.rows <= 32) shrink_many<T, NR, 2>(c, t, first, split, s0, s1, shared); else shrink_many<T, NR, 4>(c, t, first, split, s0, s1, shared); } while (0)
+#define SPQR_SHRINK(NR) do { if (t.rows <= 32) shrink_many<T, NR, 2>(c, t, tiles_of, first, end, split, s0, s1, shared); else shrink_many<T, NR, 4>(c, t, tiles_of, first, end, split, s0, s1, shared); } while (0)
   if (left <= 4) SPQR_SHRINK(1);
   else if (left <= 8) SPQR_SHRINK(2);
+  else if (left <= 12) SPQR_SHRINK(3);
   else SPQR_SHRINK(4);
 #undef SPQR_SHRINK
 }
@@ -773,12 +782,11 @@ static Call call_of(const spqr_adapters_t* a, const spqr_adapter_plan_t* plan, i
   c.x = a->x; c.x_stride = a->x_stride; c.width = a->width; c.slots = a->slots;
   c.count = plan->count; c.tile = plan->tile; c.row = plan->row; c.rows = plan->rows; c.max_tiles = c.v_tiles = tiles;
   c.v = static_cast<float*>(a->workspace);
-  int at = 0, tile = 0;
+  int at = 0;
   for (int p = 0; p < SPQR_MAX_FUSED; ++p) {
-    if (p >= a->count) { c.p[p] = Projection{}; continue; }
+    if (p >= a->count) { c.p[p] = Projection{}; c.p[p].bank = c.p[0].bank; continue; }       // (a bank to look into, of no ranks)
     c.p[p] = Projection{static_cast<const uint8_t*>(a->bank[p]), a->scale[p], a->y[p], a->out[p], a->y_stride[p], a->out_stride[p], a->m[p], a->max_rank[p], at};
     at += (a->max_rank[p] + 31) / 32;
-    for (int k = 0; k < a->max_rank[p]; k += 16) c.rank_tile[tile++] = p + 256 * (k / 16);
   }
   return c;
 }
