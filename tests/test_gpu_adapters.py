@@ -325,3 +325,67 @@ def test_refusals_of_the_binding():
         K.spqr_adapters(b, large, torch.zeros(5000, 64, dtype=torch.float16, device="cuda"))
     with pytest.raises(P.SpQRError):
         K.spqr_adapters(b, K.SpQRAdapterPlan(4, 3), x, [y])
+
+
+def some_bank(g, slots, rank, width, ms, rows, workspace=None, dtype=torch.float16):
+    make = lambda *shape: (torch.randn(shape, device="cuda", generator=g) * 0.1).to(dtype)  # noqa: E731
+    return K.SpQRAdapters([make(slots, rank, width) for _ in ms], [make(slots, m, rank) for m in ms], rows=rows, workspace=workspace)
+
+
+@pytest.mark.parametrize("rows,rank", [(3, 16), (130, 40), (130, 200)])
+def test_offsets_beyond_32_bits(rows, rank):
+    """Rows far from each other give what they give side by side, bit by bit, in place; a row of no adapter too."""
+    width, ms, stride = 260, [200, 500], 1 << (31 if rows == 3 else 25)
+    g = torch.Generator(device="cuda").manual_seed(rank)
+    bank = some_bank(g, 2, rank, width, ms, rows)
+    plan = K.spqr_adapter_plan(K.SpQRAdapterPlan(rows, 2), ints([(0, 1, -1)[r % 3] if r % 50 == 2 else r // 100 for r in range(rows)]))
+    x = torch.randn(rows, width, device="cuda", generator=g).half()
+    ys = [torch.randn(rows, m, device="cuda", generator=g).half() for m in ms]
+    want = K.spqr_adapters(bank, plan, x, ys)
+    far = torch.empty((rows - 1) * stride + 2048, dtype=torch.float16, device="cuda")
+    place = lambda at, m: torch.as_strided(far, (rows, m), (stride, 1), at)  # noqa: E731
+    places = [place(0, width), place(512, ms[0]), place(1024, ms[1])]
+    for to, t in zip(places, [x] + ys):
+        to.copy_(t)
+    got = K.spqr_adapters(bank, plan, places[0], places[1:], places[1:])
+    assert all(torch.equal(a, b) for a, b in zip(got, want)) and torch.equal(places[0], x)
+
+
+def test_banks_that_share_scratch_and_steps_of_fewer_rows():
+    """Banks called one after the other on one scratch, for steps of any size up to theirs, give what each gives on its own."""
+    g = torch.Generator(device="cuda").manual_seed(5)
+    shapes = [(64, 512, [512, 128]), (16, 512, [900]), (130, 900, [512])]
+    alone = [some_bank(g, 3, *s, rows=700) for s in shapes]
+    room = torch.empty(max(b.workspace.numel() for b in alone), dtype=torch.uint8, device="cuda")
+    g.manual_seed(5)
+    shared = [some_bank(g, 3, *s, rows=700, workspace=room) for s in shapes]
+    for rows in (1, 17, 64, 700, 129, 2):
+        plan = K.spqr_adapter_plan(K.SpQRAdapterPlan(rows, 3), ints([(r * 7 // 5) % 4 - 1 for r in range(rows)]))
+        xs = [torch.randn(rows, s[1], device="cuda", generator=g).half() for s in shapes]
+        want = [K.spqr_adapters(b, plan, x) for b, x in zip(alone, xs)]
+        room.fill_(255)                                     # (NaN)
+        got = [K.spqr_adapters(b, plan, x) for b, x in zip(shared, xs)]
+        for a, b in zip(got, want):
+            assert all(torch.equal(u, v) for u, v in zip(a, b))
+    with pytest.raises(P.SpQRError):                        # more rows than there is scratch for
+        plan = K.spqr_adapter_plan(K.SpQRAdapterPlan(5000, 3), ints([0] * 5000))
+        K.spqr_adapters(alone[0], plan, torch.zeros(5000, 512, dtype=torch.float16, device="cuda"))
+
+
+@pytest.mark.parametrize("dtype,y", [("f16", "f32"), ("bf16", "f16")])
+@pytest.mark.parametrize("m", [33, 63, 223, 300, 1751])
+@pytest.mark.parametrize("rows", [5, 100, 700])
+def test_the_ends_of_rows_stay_in_their_rows(rows, m, dtype, y):
+    """Outputs whose rows lie side by side in a wider tensor, at odd places: the elements between them stay, long ranks and short ones."""
+    for rank in (8, 64, 72, 200):
+        g = torch.Generator(device="cuda").manual_seed(rank + m)
+        bank = some_bank(g, 2, rank, 300, [m], rows, dtype=TYPES[dtype])
+        plan = K.spqr_adapter_plan(K.SpQRAdapterPlan(rows, 2), ints([r % 3 - 1 for r in range(rows)]))
+        x = torch.randn(rows, 300, device="cuda", generator=g).to(TYPES[dtype])
+        base = torch.randn(rows, m, device="cuda", generator=g).to(TYPES[y])
+        want, = K.spqr_adapters(bank, plan, x, [base])
+        wide = torch.full((rows, m + 7), 3.0, dtype=TYPES[y], device="cuda")
+        into = wide[:, 3:3 + m]
+        into.copy_(base)
+        K.spqr_adapters(bank, plan, x, [into], [into])
+        assert torch.equal(into, want) and bool((wide[:, :3] == 3.0).all()) and bool((wide[:, 3 + m:] == 3.0).all())

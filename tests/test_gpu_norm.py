@@ -216,3 +216,21 @@ def test_another_stream_and_a_captured_call():
     graph.replay()
     torch.cuda.synchronize()
     assert torch.equal(total, want2[0]) and torch.equal(out, want2[1])
+
+
+@pytest.mark.parametrize("rows,stride", [(3, 1 << 31), (4200, (1 << 20) + 8)])
+def test_offsets_beyond_32_bits(rows, stride):
+    """Rows far from each other give what they give side by side, bit by bit; what lies between them stays."""
+    width = 1024
+    g = torch.Generator(device="cuda").manual_seed(rows)
+    norm = K.SpQRResidualNorm(width, norm_y="layer", act="sigmoid", out_dtype="bfloat16")
+    far = torch.empty((rows - 1) * stride + 4 * width, dtype=torch.bfloat16, device="cuda")
+    place = lambda at: torch.as_strided(far, (rows, width), (stride, 1), at * width)  # noqa: E731
+    x, y, gate = (torch.randn(rows, width, device="cuda", generator=g).bfloat16() for _ in range(3))
+    want_sum, want = K.spqr_residual_norm(norm, x, y, gate)
+    for at, t in enumerate((x, y, gate)):
+        place(at).copy_(t)
+    place(3).fill_(7.0)
+    got_sum, got = K.spqr_residual_norm(norm, place(0), place(1), place(2), sum=place(0), out=place(3))
+    assert torch.equal(got_sum, want_sum) and torch.equal(got, want)
+    assert torch.equal(place(1), y) and torch.equal(place(2), gate)
