@@ -7,6 +7,7 @@ constexpr float kLog2e = 1.44269504088896341f;
 constexpr int kCandidates = 2048;                // logits that can be among the best which there is room for
 constexpr int kJoined = 1024;                    // keys of the parts of a row
 constexpr int kPartGroups = 512, kShortest = 4096;         // rows are cut for so many workgroups, parts no shorter than this
+constexpr int kResident = 1024, kMiddling = 49152;         // workgroups of 512 threads that run at once; rows that 256 threads take where there are more
 
 // c = scale * log2(e), as binary32: probabilities go by powers of two, 2^(l c - ref) over their sum.  A thread's reference is a whole number near its
 // largest l c, so that one fused multiply and subtract gives l c - ref with one rounding; sums of another reference move by a power of two.
@@ -358,7 +359,9 @@ static int launch_score(const spqr_token_logprobs_t& p, hipStream_t st) {
   Part* parts = static_cast<Part*>(p.workspace);
   uint64_t* keys = reinterpret_cast<uint64_t*>(parts + (int64_t)p.rows * cut.parts);
   if (cut.parts == 1) {
-    if (p.vocab <= 8192) hipLaunchKernelGGL((score_kernel<T, 256, true>), dim3(p.rows), dim3(256), 0, st, p, p.vocab, nullptr, nullptr);
+    // 256 threads where a row is short, or where rows are more than 512 threads each have room for at once and not so long that the row's length is all
+    // that counts: 2048 rows of 10001 20 us (512 threads: 28), of 32000 39 (45), of 48000 54 (57), but of 65537 80 (74); 600 rows of 32000 22 (19), 1024 of 40000 42 (38).
+    if (p.vocab <= 8192 || (p.rows > kResident && p.vocab <= kMiddling)) hipLaunchKernelGGL((score_kernel<T, 256, true>), dim3(p.rows), dim3(256), 0, st, p, p.vocab, nullptr, nullptr);
     else hipLaunchKernelGGL((score_kernel<T, 512, true>), dim3(p.rows), dim3(512), 0, st, p, p.vocab, nullptr, nullptr);
     return launched();
   }

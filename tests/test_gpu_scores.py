@@ -82,6 +82,13 @@ def test_rows(rows):
         check(logits, tokens(1), 5)
 
 
+@pytest.mark.parametrize("rows,vocab", [(1024, 20001), (1025, 20001), (1100, 8193), (1030, 49152), (1030, 49153)])
+def test_many_rows_of_middling_length(rows, vocab):
+    g = torch.Generator(device="cuda").manual_seed(vocab)
+    logits = (torch.randn(rows, vocab, device="cuda", generator=g) * 3).half()
+    check(logits, torch.randint(0, vocab, (rows, 2), dtype=torch.int32, device="cuda", generator=g), 7)
+
+
 @pytest.mark.parametrize("top", [0, 1, 2, 5, 16, 31, 32, 33, 63, 64])
 def test_alternatives(top):
     for rows, vocab in ((1, 32000), (5, 70000), (40, 3001), (3, 40)):
