@@ -11,9 +11,11 @@ constexpr int kResident = 1024, kMiddling = 49152;         // workgroups of 512 
 
 // c = scale * log2(e), as binary32: probabilities go by powers of two, 2^(l c - ref) over their sum.  A thread's reference is a whole number near its
 // largest l c, so that one fused multiply and subtract gives l c - ref with one rounding; sums of another reference move by a power of two.
-// It moves up when a logit passes it by 2^8.  Where the largest l c is beyond 2^100 (or has no number), a loop that subtracts the largest logit
-// first takes the row again.
-constexpr float kFar = 1.2676506e30f;            // 2^100
+// It moves up when a logit passes it by 2^8, and never lies below -2^24.  Where the largest l c is 2^24 or more in size (or has no number), a loop that
+// subtracts the largest logit first takes the row again: there l c has no bits below 1, its rounding (128 and more from 2^31 on) would be a power of
+// two by itself.  For the same reason a thread whose logits all lie below -2^24 (masks by -1e10 and the like) keeps the lowest reference:
+// theirs are powers of two that are 0 beside any other logit.
+constexpr float kFar = 16777216.f;               // 2^24
 constexpr double kLn2 = 0.693147180559945309;
 
 struct Soft { float ref, sum, dot; };            // sum of 2^(l c - ref), of (l c - ref) 2^(l c - ref)
