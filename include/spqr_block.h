@@ -166,8 +166,8 @@ typedef struct spqr_token_logprobs_t {
 int64_t spqr_token_logprobs_workspace_bytes(const spqr_token_logprobs_t* p);
 
 /* Logits of -infinity are tokens of probability 0 (log probability -infinity, nothing in the entropy); a row that has only
- * such: entropy 0.  The type's lowest finite value is a logit like others.  A row with a NaN or +infinity: its logprob, entropy and
- * top_logprob are NaN; its top_token are by value, NaN left out. */
+ * such: entropy 0.  The type's lowest finite value is a logit like others.  A row with a NaN or +infinity: its logprob (of tokens in
+ * [0, vocab)), entropy and all of its top_logprob are NaN; its top_token are by value, NaN left out, -1 behind the last. */
 int spqr_token_logprobs(const spqr_token_logprobs_t* p, void* stream);
 
 #ifdef __cplusplus

@@ -109,7 +109,8 @@ __device__ __forceinline__ void write_top(const spqr_token_logprobs_t& p, int64_
     const uint64_t key = i < count ? best[i] : 0;
     const int64_t at = r * p.top + i;
     p.top_token[at] = i < count ? (int32_t)~(uint32_t)key : -1;
-    p.top_logprob[at] = i < count ? row.logprob(unordered((uint32_t)(key >> 32))) : -INFINITY;
+    // (a row with a NaN or +infinity has no log probabilities, in places without a token neither)
+    p.top_logprob[at] = i < count ? row.logprob(unordered((uint32_t)(key >> 32))) : row.soft.sum != row.soft.sum ? NAN : -INFINITY;
   }
 }
 
