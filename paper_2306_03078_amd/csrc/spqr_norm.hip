@@ -118,6 +118,14 @@ __device__ __forceinline__ float squares_of(const float (&v)[CH][8], const Place
   return sum;
 }
 
+// 1 / sqrt(v), v > 0.  The card's instruction takes subnormal numbers for 0 (an eps below 2^-126, of rows of zeros): they are taken 2^64 times
+// as large.
+__device__ __forceinline__ float inverse_root(float v) {
+  const bool small = v < 0x1p-126f;
+  const float r = __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v);
+  return small ? r * 0x1p32f : r;
+}
+
 template <bool ODD, int CH>
 __device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Place (&at)[CH], const spqr_residual_norm_t& p, const void* weight, const void* bias,
                                           const Raw (&w)[CH], const Raw (&b)[CH], RowSum& sum) {
@@ -130,7 +138,7 @@ __device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Pla
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] -= mean;
   }
-  const float r = __builtin_amdgcn_rsqf(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
+  const float r = inverse_root(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     float x[8], y[8];
