@@ -356,6 +356,20 @@ static int check_scores(const spqr_token_logprobs_t* p) {
   return SPQR_OK;
 }
 
+// Rows of one launch: 2^31 threads (a grid of 2^32 threads in one direction loses what is beyond them, without an error).
+constexpr int kMostRows = 1 << 22;
+
+template <typename T>
+static spqr_token_logprobs_t rows_from(const spqr_token_logprobs_t& p, int64_t from) {
+  spqr_token_logprobs_t q = p;
+  q.rows = p.rows - from < kMostRows ? (int)(p.rows - from) : kMostRows;
+  q.logits = static_cast<const T*>(p.logits) + from * p.stride;
+  if (p.given > 0) { q.tokens = p.tokens + from * p.given; q.logprob = p.logprob + from * p.given; }
+  if (p.entropy) q.entropy = p.entropy + from;
+  if (p.top > 0) { q.top_token = p.top_token + from * p.top; q.top_logprob = p.top_logprob + from * p.top; }
+  return q;
+}
+
 template <typename T>
 static int launch_score(const spqr_token_logprobs_t& p, hipStream_t st) {
   const Cut cut = cut_of(p.rows, p.vocab, p.top);
@@ -364,8 +378,12 @@ static int launch_score(const spqr_token_logprobs_t& p, hipStream_t st) {
   if (cut.parts == 1) {
     // 256 threads where a row is short, or where rows are more than 512 threads each have room for at once and not so long that the row's length is all
     // that counts: 2048 rows of 10001 20 us (512 threads: 28), of 32000 39 (45), of 48000 54 (57), but of 65537 80 (74); 600 rows of 32000 22 (19), 1024 of 40000 42 (38).
-    if (p.vocab <= 8192 || (p.rows > kResident && p.vocab <= kMiddling)) hipLaunchKernelGGL((score_kernel<T, 256, true>), dim3(p.rows), dim3(256), 0, st, p, p.vocab, nullptr, nullptr);
-    else hipLaunchKernelGGL((score_kernel<T, 512, true>), dim3(p.rows), dim3(512), 0, st, p, p.vocab, nullptr, nullptr);
+    const bool small = p.vocab <= 8192 || (p.rows > kResident && p.vocab <= kMiddling);
+    for (int64_t from = 0; from < p.rows; from += kMostRows) {
+      const spqr_token_logprobs_t q = rows_from<T>(p, from);
+      if (small) hipLaunchKernelGGL((score_kernel<T, 256, true>), dim3(q.rows), dim3(256), 0, st, q, q.vocab, nullptr, nullptr);
+      else hipLaunchKernelGGL((score_kernel<T, 512, true>), dim3(q.rows), dim3(512), 0, st, q, q.vocab, nullptr, nullptr);
+    }
     return launched();
   }
   hipLaunchKernelGGL((score_kernel<T, 256, false>), dim3(p.rows, cut.parts), dim3(256), 0, st, p, cut.length, parts, keys);
