@@ -318,13 +318,13 @@ __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at
   }
 }
 
-// `lanes` threads a row, CH runs of eight elements each, which stay in registers from the loads to the stores.
+// `lanes` threads a row, CH runs of eight elements each, which stay in registers from the loads to the stores.  first: of the launch's workgroups.
 template <int CH>
-__global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_t p, int lanes) {
+__global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_t p, int lanes, int64_t first) {
   __shared__ __align__(16) float part[2][16];
   RowSum row_sum{part, lanes, 0};
   const int n = p.width, in_row = threadIdx.x & (lanes - 1);
-  const int64_t row = (int64_t)blockIdx.x * (blockDim.x / lanes) + threadIdx.x / lanes;
+  const int64_t row = (first + blockIdx.x) * (blockDim.x / lanes) + threadIdx.x / lanes;
   const bool live = row < p.rows;
   const int64_t t = live ? row : p.rows - 1;               // (takes part in the sums, stores nothing)
   int at[CH];
@@ -416,7 +416,6 @@ extern "C" int spqr_residual_norm(const spqr_residual_norm_t* p, void* stream) {
   while (lanes < runs && lanes < 1024) lanes *= 2;
   const int threads = lanes > 256 ? lanes : 256, per = threads / lanes;
   const int64_t grid = ((int64_t)p->rows + per - 1) / per;
-  const dim3 g((unsigned)grid), b(threads);
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int ch = (runs + lanes - 1) / lanes;
   if (ch <= 1 && p->width >= 8) {
@@ -425,9 +424,13 @@ extern "C" int spqr_residual_norm(const spqr_residual_norm_t* p, void* stream) {
     else launch_rows_any<__bf16>(*p, lanes, threads, grid, st);
     return launched();
   }
-  if (ch <= 1) hipLaunchKernelGGL(residual_norm_kernel<1>, g, b, 0, st, *p, lanes);
-  else if (ch <= 2) hipLaunchKernelGGL(residual_norm_kernel<2>, g, b, 0, st, *p, lanes);
-  else if (ch <= 4) hipLaunchKernelGGL(residual_norm_kernel<4>, g, b, 0, st, *p, lanes);
-  else hipLaunchKernelGGL(residual_norm_kernel<8>, g, b, 0, st, *p, lanes);
+  // 2^31 threads a launch (a grid of 2^32 threads in one direction loses what is beyond them, without an error)
+  for (int64_t first = 0; first < grid; first += 1 << 21) {
+    const dim3 g((unsigned)(grid - first < 1 << 21 ? grid - first : 1 << 21)), b(threads);
+    if (ch <= 1) hipLaunchKernelGGL(residual_norm_kernel<1>, g, b, 0, st, *p, lanes, first);
+    else if (ch <= 2) hipLaunchKernelGGL(residual_norm_kernel<2>, g, b, 0, st, *p, lanes, first);
+    else if (ch <= 4) hipLaunchKernelGGL(residual_norm_kernel<4>, g, b, 0, st, *p, lanes, first);
+    else hipLaunchKernelGGL(residual_norm_kernel<8>, g, b, 0, st, *p, lanes, first);
+  }
   return launched();
 }
