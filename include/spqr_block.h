@@ -78,7 +78,7 @@ typedef struct spqr_adapter_plan_t {
   int32_t slots;                 /* 1 .. SPQR_MAX_SLOTS                                                                 */
   int32_t requests;              /* entries of adapter, 0 .. SPQR_MAX_REQUESTS; without q_start: = rows                 */
   int32_t max_tiles;             /* of tile and row; spqr_adapter_tiles(rows, slots) or more                            */
-  const int32_t* adapter;        /* [requests]                                                                          */
+  const int32_t* adapter;        /* [requests]; NULL with requests 0: every row is in no tile                           */
   const int32_t* q_start;        /* [requests + 1], ascending, or NULL                                                  */
   int32_t* count;                /* [1] tiles in use                                                                    */
   int32_t* tile;                 /* [max_tiles][2] slot (-1: rows of no adapter), rows; -1, 0 behind the last           */

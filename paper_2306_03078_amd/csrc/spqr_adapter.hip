@@ -845,7 +845,7 @@ extern "C" int spqr_adapter_plan(const spqr_adapter_plan_t* p, void* stream) {
   if (rc) return rc;
   if (p->q_start ? p->requests < 0 || p->requests > SPQR_MAX_REQUESTS : p->requests != p->rows) return SPQR_ERR_SHAPE;
   if (p->rows == 0) return SPQR_OK;
-  if (!p->adapter) return SPQR_ERR_NULL;
+  if (!p->adapter && p->requests > 0) return SPQR_ERR_NULL;      // (an array of nothing has no address)
   if (!aligned(p->adapter, 4) || !aligned(p->q_start, 4)) return SPQR_ERR_ALIGN;
   const dim3 grid(p->slots + 1);
   const hipStream_t st = static_cast<hipStream_t>(stream);
