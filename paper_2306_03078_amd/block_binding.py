@@ -1,7 +1,10 @@
 """ctypes binding of what a decoder's step does beside its products and its attention (include/spqr_block.h): argument marshalling only.
 
 Each operator has a handle with what a program keeps from call to call (weights, sizes, scratch, small outputs); every computation
-runs in the library's kernels.  No CPU fallback: a missing libspqr.so raises.  A handle is used on one stream at a time.
+runs in the library's kernels.  No CPU fallback: a missing libspqr.so raises.  A handle is used on one stream at a time, and stays until
+its last call has run; what its constructor does is done when it returns, so that the first call may be on any stream.  stream: that of
+the call, None for the current one; tensors that a call makes are that stream's, as under torch.cuda.stream(stream); those that it is given are
+ready there, and stay until it has run (Tensor.record_stream), as with torch's own calls.
 """
 from __future__ import annotations
 
@@ -72,15 +75,32 @@ def _lib():
     return lib
 
 
-def _run(name, index, stream, desc, *args):
-    """One of the entries, on the handle's device: launches go to the current one, on its current stream where none is given."""
+def _run(name, index, desc, *args):
+    """One of the entries, on the handle's device: launches go to the current one, on its current stream."""
     if S._current_device() != index:
         import torch
         with torch.cuda.device(index):
-            return _run(name, index, stream, desc, *args)
-    rc = B._call(_entry[name], desc, *args, S._raw_stream(index) if stream is None else stream.cuda_stream)
+            return _run(name, index, desc, *args)
+    rc = B._call(_entry[name], desc, *args, S._raw_stream(index))
     if rc != 0:
         raise SpQRError(int(rc), name)
+
+
+def _on(stream, index):
+    """A call's stream as the current one: memory that torch gives for what the call makes is then ordered with its kernels."""
+    import torch
+    if stream.device_index != index:
+        raise ValueError(f"a stream of cuda:{stream.device_index} for a handle on cuda:{index}")
+    return torch.cuda.stream(stream)
+
+
+def _wait_for(device):
+    """What a constructor did on the current stream, and kernels there that still use the memory that it was given, before calls on other streams.
+    (In a capture the graph has the order.)"""
+    import torch
+    with torch.cuda.device(device):
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
 
 
 def _device(device):
@@ -144,6 +164,9 @@ def spqr_residual_norm(norm: SpQRResidualNorm, x=None, y=None, gate=None, *, sum
     made where there are both x and y, or written to `sum` (which may be x); else None.  The norm, of the handle's out_dtype, is made or
     written to `out`; None with out_dtype None."""
     index, dtypes = norm._index, S._dtypes
+    if stream is not None:
+        with _on(stream, index):
+            return spqr_residual_norm(norm, x, y, gate, sum=sum, out=out)
     rows = y if x is None else x
     if rows is None or rows.dim() != 2:
         raise ValueError("x, y: [rows, width], one of them at least")
@@ -184,7 +207,7 @@ def spqr_residual_norm(norm: SpQRResidualNorm, x=None, y=None, gate=None, *, sum
     d = norm.desc
     _norm_types.pack_into(d, 0, count, width, x_type, y_type, gate_type, norm._out_type)
     _norm_rows.pack_into(d, _norm_rows_at, x_at, y_at, gate_at, sum_at, out_at, x_stride, y_stride, sum_stride, out_stride, gate_stride)
-    _run("spqr_residual_norm", index, stream, d)
+    _run("spqr_residual_norm", index, d)
     return sum, out
 
 
@@ -207,17 +230,21 @@ class SpQRAdapterPlan:
         d = self.desc = spqr_adapter_plan_t(rows=self.rows, slots=self.slots, max_tiles=tiles, count=self.count.data_ptr(), tile=self.tile.data_ptr(),
                                             row=self.row.data_ptr())
         self._at = C.addressof(d)
+        _wait_for(self.device)
 
 
 def spqr_adapter_plan(plan: SpQRAdapterPlan, adapter, q_start=None, stream=None) -> SpQRAdapterPlan:
     """The step's rows by adapter.  adapter: int32 [requests], the slot of each request (anything outside: none), with q_start int32
     [requests + 1] (SpQRStep.q_start); or [rows], without."""
     d, index = plan.desc, plan._index
+    if stream is not None:
+        with _on(stream, index):
+            return spqr_adapter_plan(plan, adapter, q_start)
     for name, a, n in (("adapter", adapter, plan.rows if q_start is None else adapter.numel()), ("q_start", q_start, adapter.numel() + 1)):
         if a is not None and (a.dtype != S._int32 or not a.is_contiguous() or a.dim() != 1 or a.numel() != n or a.get_device() != index):
             raise ValueError(f"{name}: a contiguous int32 tensor [{n}] on {plan.device}, not {a.dtype} {list(a.shape)} on {a.device}")
     d.requests, d.adapter, d.q_start = adapter.numel(), adapter.data_ptr(), None if q_start is None else q_start.data_ptr()
-    _run("spqr_adapter_plan", index, stream, d)
+    _run("spqr_adapter_plan", index, d)
     return plan
 
 
@@ -269,12 +296,21 @@ class SpQRAdapters:
         self.workspace = workspace
         d.workspace, d.workspace_bytes = workspace.data_ptr(), workspace.numel() * workspace.element_size()
         self.load(0, A, B, rank)
+        _wait_for(self.device)
 
     def load(self, first, A, B, rank=None, stream=None):
-        """Other adapters into the slots from `first` on: A, B and rank as above, of as many slots as are to be filled."""
+        """Other adapters into the slots from `first` on: A, B and rank as above, of as many slots as are to be filled (not needed after the call,
+        on another stream neither)."""
         import torch
         k, A, B = len(self.m), list(A), list(B)
         rank = [rank] * k if rank is None or hasattr(rank, "dtype") else list(rank)
+        if stream is not None:
+            with _on(stream, self._index):
+                self.load(first, A, B, rank)
+            for t in A + B + rank:
+                if t is not None:
+                    t.record_stream(stream)
+            return
         if len(A) != k or len(B) != k or len(rank) != k:
             raise ValueError(f"A, B: {k} tensors; rank: one, or {k}")
         slots = A[0].shape[0]
@@ -289,7 +325,7 @@ class SpQRAdapters:
                 raise ValueError(f"rank: a contiguous int32 tensor [{slots}] on {self.device}")
         lib = _lib()
         with torch.cuda.device(self._index):
-            to = S._raw_stream(self._index) if stream is None else stream.cuda_stream
+            to = S._raw_stream(self._index)
             for p in range(k):
                 rc = lib.spqr_adapters_pack(C.byref(self.desc), p, first, slots, A[p].data_ptr(), B[p].data_ptr(), None if rank[p] is None else rank[p].data_ptr(), to)
                 if rc != 0:
@@ -301,6 +337,9 @@ def spqr_adapters(bank: SpQRAdapters, plan: SpQRAdapterPlan, x, ys=None, outs=No
     [rows, m[p]] of one type.  ys None: zeros (outs are float32 unless given).  outs None: new tensors; outs may be ys.  Rows that the
     plan has in no tile are left as they are."""
     d, index, dtypes = bank.desc, bank._index, S._dtypes
+    if stream is not None:
+        with _on(stream, index):
+            return spqr_adapters(bank, plan, x, ys, outs)
     rows, k, ms = plan.rows, len(bank.m), bank.m
     if plan._index != index:
         raise ValueError(f"a plan on {plan.device}, banks on {bank.device}")
@@ -327,7 +366,7 @@ def spqr_adapters(bank: SpQRAdapters, plan: SpQRAdapterPlan, x, ys=None, outs=No
         fields[SPQR_MAX_FUSED + p] = outs[p].data_ptr()
     _bank_rows.pack_into(d, _bank_rows_at, *fields)
     d.y_dtype = dtypes[dtype]
-    _run("spqr_adapters", index, stream, d, plan._at)
+    _run("spqr_adapters", index, d, plan._at)
     return outs
 
 
@@ -351,12 +390,16 @@ class SpQRScores:
         self.top_token, self.top_logprob = empty(self.rows, self.top, dtype=torch.int32), empty(self.rows, self.top)
         for n in ("logprob", "entropy", "top_token", "top_logprob"):
             setattr(d, n, getattr(self, n).data_ptr())
+        _wait_for(self.device)
 
 
 def spqr_token_logprobs(scores: SpQRScores, logits, tokens=None, scale: float = 1.0, stream=None) -> SpQRScores:
     """Fills `scores` for logits [rows, vocab] (float32, float16, bfloat16): log softmax(scale * logits) of tokens int32 [rows, given]
     ([rows] where given is 1), entropies, the most probable tokens.  Fewer rows than the handle's: the first ones are filled."""
     d, index = scores.desc, scores._index
+    if stream is not None:
+        with _on(stream, index):
+            return spqr_token_logprobs(scores, logits, tokens, scale)
     if logits.dim() != 2 or logits.shape[0] > scores.rows:
         raise ValueError(f"logits: up to {scores.rows} rows of {scores.vocab}, not {list(logits.shape)}")
     rows = logits.shape[0]
@@ -368,5 +411,5 @@ def spqr_token_logprobs(scores: SpQRScores, logits, tokens=None, scale: float = 
     elif tokens is not None:
         raise ValueError("tokens: this handle has given = 0")
     d.scale = scale
-    _run("spqr_token_logprobs", index, stream, d)
+    _run("spqr_token_logprobs", index, d)
     return scores
