@@ -1,7 +1,8 @@
 """ctypes binding of the C ABI declared in include/spqr.h (same names).
 
 Argument marshalling only.  There is no CPU fallback: if libspqr.so is missing
-the first call raises.
+the first call raises.  stream: that of a call, None for the current one; tensors that a call makes are that stream's, as under
+torch.cuda.stream(stream); those that it is given are ready there, and stay until it has run, as with torch's own calls.
 """
 from __future__ import annotations
 
@@ -184,6 +185,23 @@ def _stream_ptr(stream) -> Optional[int]:
     return torch.cuda.current_stream().cuda_stream
 
 
+def _on(stream):
+    """A call's stream as the current one: memory that torch gives for what the call makes (results, scratch) is then ordered with its
+    kernels.  (Of the current stream's memory, work that is still to run there could write to it, and what is let go early is given out again
+    before the kernels have read it.)"""
+    import torch
+    return torch.cuda.stream(stream)
+
+
+def _wait_for(device):
+    """What a constructor did on the current stream, and kernels there that still use the memory that it was given, before calls on other streams.
+    (In a capture the graph has the order.)"""
+    import torch
+    with torch.cuda.device(device):
+        if not torch.cuda.is_current_stream_capturing():
+            torch.cuda.current_stream().synchronize()
+
+
 class SpQRMatrix:
     """Device-resident SpQR matrix: torch tensors own the memory, the
     descriptor points into them."""
@@ -258,6 +276,9 @@ def _out_dtype(y_dtype):
 
 def spqr_gemv(A: SpQRMatrix, x, out=None, y_dtype: int = SPQR_F32, stream=None):
     """y[m] = W_hat . x, x: float16 device tensor [n]."""
+    if stream is not None and out is None:
+        with _on(stream):
+            return spqr_gemv(A, x, out, y_dtype)
     if _lib is None:
         load_library()
     assert x.dtype == _half and x.is_contiguous() and x.numel() == A.n
@@ -273,6 +294,9 @@ def spqr_gemv(A: SpQRMatrix, x, out=None, y_dtype: int = SPQR_F32, stream=None):
 
 def spqr_gemm_smallbatch(A: SpQRMatrix, X, out=None, y_dtype: int = SPQR_F32, stream=None):
     """Y[b, m] = X[b, :] . W_hat^T, X: float16 device tensor [b, n], 1 <= b <= SPQR_MAX_BATCH (256)."""
+    if stream is not None and out is None:
+        with _on(stream):
+            return spqr_gemm_smallbatch(A, X, out, y_dtype)
     import torch
     assert X.dtype == torch.float16 and X.is_contiguous() and X.dim() == 2 and X.shape[1] == A.n
     b = int(X.shape[0])
@@ -287,6 +311,9 @@ def spqr_gemm_smallbatch(A: SpQRMatrix, X, out=None, y_dtype: int = SPQR_F32, st
 
 def spqr_gemv_fused(As, x, outs=None, y_dtype: int = SPQR_F32, stream=None):
     """y_i[m_i] = W_hat_i . x for matrices sharing the input vector; one launch when possible."""
+    if stream is not None and outs is None:
+        with _on(stream):
+            return spqr_gemv_fused(As, x, outs, y_dtype)
     import torch
     As = list(As)
     assert x.dtype == torch.float16 and x.is_contiguous() and x.numel() == As[0].n
@@ -302,6 +329,9 @@ def spqr_gemv_fused(As, x, outs=None, y_dtype: int = SPQR_F32, stream=None):
 
 def spqr_gemm_fused(As, X, outs=None, y_dtype: int = SPQR_F32, stream=None):
     """Y_i[b, m_i] = X[b, :] . W_hat_i^T for matrices sharing the batch X (float16 device tensor [b, n])."""
+    if stream is not None and outs is None:
+        with _on(stream):
+            return spqr_gemm_fused(As, X, outs, y_dtype)
     import torch
     As = list(As)
     assert X.dtype == torch.float16 and X.is_contiguous() and X.dim() == 2 and X.shape[1] == As[0].n
@@ -340,6 +370,9 @@ def _ws_args(workspace):
 
 def spqr_gemm_smallbatch_ws(A: SpQRMatrix, X, workspace, out=None, y_dtype: int = SPQR_F32, stream=None):
     """spqr_gemm_smallbatch with scratch in `workspace` (a device tensor, or None where none is needed)."""
+    if stream is not None and out is None:
+        with _on(stream):
+            return spqr_gemm_smallbatch_ws(A, X, workspace, out, y_dtype)
     import torch
     assert X.dtype == torch.float16 and X.is_contiguous() and X.dim() == 2 and X.shape[1] == A.n
     b = int(X.shape[0])
@@ -355,6 +388,9 @@ def spqr_gemm_smallbatch_ws(A: SpQRMatrix, X, workspace, out=None, y_dtype: int 
 
 def spqr_gemm_fused_ws(As, X, workspace, outs=None, y_dtype: int = SPQR_F32, stream=None):
     """spqr_gemm_fused with scratch in `workspace`."""
+    if stream is not None and outs is None:
+        with _on(stream):
+            return spqr_gemm_fused_ws(As, X, workspace, outs, y_dtype)
     import torch
     As = list(As)
     assert X.dtype == torch.float16 and X.is_contiguous() and X.dim() == 2 and X.shape[1] == As[0].n
@@ -381,6 +417,9 @@ def spqr_gemm_smallbatch_noalloc(A: SpQRMatrix, X, out, y_dtype: int = SPQR_F32,
 
 def spqr_gemv_grouped(As, xs, outs=None, y_dtype: int = SPQR_F32, stream=None):
     """y_i[m_i] = W_hat_i . x_i for matrices with an input vector each; as few launches as possible."""
+    if stream is not None and outs is None:
+        with _on(stream):
+            return spqr_gemv_grouped(As, xs, outs, y_dtype)
     import torch
     As, xs = list(As), list(xs)
     assert len(As) == len(xs)
@@ -398,6 +437,9 @@ def spqr_gemv_grouped(As, xs, outs=None, y_dtype: int = SPQR_F32, stream=None):
 
 def spqr_dequant_dense(A: SpQRMatrix, what: int, stream=None):
     """Debug decode; returns a new device tensor shaped for the selector."""
+    if stream is not None:
+        with _on(stream):
+            return spqr_dequant_dense(A, what)
     import torch
     sel = what & 0xFF
     gshape = (A.m, A.n // A.beta1) if A.group_axis == 0 else (A.m // A.beta1, A.n)

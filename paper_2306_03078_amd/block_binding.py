@@ -13,7 +13,7 @@ from struct import Struct
 
 from . import binding as B
 from . import serve_binding as S
-from .binding import SpQRError
+from .binding import SpQRError, _wait_for
 from .serve_binding import SPQR_MAX_REQUESTS
 
 SPQR_MAX_WIDTH, SPQR_MAX_FUSED = 65536, 8
@@ -87,20 +87,10 @@ def _run(name, index, desc, *args):
 
 
 def _on(stream, index):
-    """A call's stream as the current one: memory that torch gives for what the call makes is then ordered with its kernels."""
-    import torch
+    """A call's stream as the current one, for what the call makes (binding._on); of the handle's device."""
     if stream.device_index != index:
         raise ValueError(f"a stream of cuda:{stream.device_index} for a handle on cuda:{index}")
-    return torch.cuda.stream(stream)
-
-
-def _wait_for(device):
-    """What a constructor did on the current stream, and kernels there that still use the memory that it was given, before calls on other streams.
-    (In a capture the graph has the order.)"""
-    import torch
-    with torch.cuda.device(device):
-        if not torch.cuda.is_current_stream_capturing():
-            torch.cuda.current_stream().synchronize()
+    return B._on(stream)
 
 
 def _device(device):

@@ -85,7 +85,8 @@ class SpQRStep:
     empty table with a ring that has all pages (pool and ends are only made with a table).  parent (int32 [tokens]) is None
     unless given, mask exists where mask_words > 0 or it is given.  rotary: float32 [positions, rotary_dim], cosines, then
     sines, or None.  scale: head_dim ** -0.5 if None.
-    The step keeps the tensors alive and owns the attention's scratch: use it on one stream at a time."""
+    The step keeps the tensors alive and owns the attention's scratch: use it on one stream at a time (the first call may be on any: what the
+    constructor does is done when it returns)."""
 
     def __init__(self, k_cache, v_cache, heads=1, *, requests=None, tokens=None, max_pages=None, page=None, pages=None, mask_words=None,
                  rotary=None, rotary_pairs=False, scale=None, max_fresh=0, device="cuda", **arrays):
@@ -182,6 +183,7 @@ class SpQRStep:
         self._q_of = torch.empty(1, dtype=self.dtype, device=self.device).expand(T, self.heads, D)
         self._rows = spqr_rows_t()
         self._rows_at = C.addressof(self._rows)
+        B._wait_for(self.device)
 
     def advance(self):
         """The next step's lengths and pages are this one's results: cached and cached_out, held and held_out, ends and
@@ -221,6 +223,9 @@ def _row_stride(x, like, name):
 def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=None):
     """q turned by its rows' positions (a tensor of the cache's type [tokens, heads, head_dim], returned); k turned, and v,
     stored in their slots of `layer`.  q, k, v: float32, float16 or bfloat16, rows of one step's products."""
+    if stream is not None and out is None:
+        with B._on(stream):
+            return spqr_cache_store(step, q, k, v, layer, out)
     x = step._rows
     dtype = q.dtype
     if dtype not in _dtypes or k.dtype != dtype or v.dtype != dtype:
@@ -241,6 +246,9 @@ def spqr_cache_store(step: SpQRStep, q, k, v, layer: int = 0, out=None, stream=N
 def spqr_tree_attention(step: SpQRStep, q, layer: int = 0, out=None, stream=None):
     """Attention of the step's rows q [tokens, heads, head_dim] (the cache's type) over the cached tokens of their requests and
     the new ones that their masks show; out has q's shape (rows that belong to no request are left as they are)."""
+    if stream is not None and out is None:
+        with B._on(stream):
+            return spqr_tree_attention(step, q, layer, out)
     if q.dtype != step.dtype:
         raise ValueError(f"q: {step.dtype}, not {q.dtype}")
     q_stride = _row_stride(q, step._q_like, "q")
