@@ -395,7 +395,8 @@ def spqr_token_logprobs(scores: SpQRScores, logits, tokens=None, scale: float = 
     rows = logits.shape[0]
     d.stride, d.dtype, d.logits, d.rows = _stride("logits", logits, (rows, scores.vocab), index), S._dtypes[logits.dtype], logits.data_ptr(), rows
     if scores.given:
-        if tokens is None or tokens.dtype != S._int32 or tokens.numel() != rows * scores.given or not tokens.is_contiguous() or tokens.get_device() != index:
+        if (tokens is None or tokens.dtype != S._int32 or tokens.numel() != rows * scores.given or not tokens.is_contiguous() or tokens.get_device() != index
+                or (scores.given > 1 and tokens.dim() == 2 and tokens.shape[0] != rows)):
             raise ValueError(f"tokens: a contiguous int32 tensor [{rows}, {scores.given}] on {scores.device}")
         d.tokens = tokens.data_ptr()
     elif tokens is not None:
