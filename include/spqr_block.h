@@ -58,9 +58,10 @@ typedef struct spqr_residual_norm_t {
   const void *y_weight, *y_bias, *x_weight, *x_bias;    /* [width]                                                       */
 } spqr_residual_norm_t;
 
-/* Statistics are of the binary32 values of s before they are rounded to sum; sums of squares must not pass binary32
- * (values below 1e17 in magnitude never do).  A row with an infinity or NaN gives NaN in that row only.  sum may be x
- * (same address and stride); sum and out overlap nothing else that is read or written. */
+/* Statistics are of the binary32 values of s before they are rounded to sum; a row's sum of squares must not pass binary32
+ * (it does not where the largest magnitude times sqrt(width) is below 1.8e19: 1.9e17 at a width of 8192, 7e16 at 65536).
+ * A row with an infinity or NaN gives NaN in that row only.  sum may be x (same address and stride); sum and out overlap
+ * nothing else that is read or written. */
 int spqr_residual_norm(const spqr_residual_norm_t* p, void* stream);
 
 /* ---- low-rank adapters of many requests ------------------------------------- */
