@@ -118,14 +118,6 @@ __device__ __forceinline__ float squares_of(const float (&v)[CH][8], const Place
   return sum;
 }
 
-// 1 / sqrt(v), v > 0.  The card's instruction takes subnormal numbers for 0 (an eps below 2^-126, of rows of zeros): they are taken 2^64 times
-// as large.
-__device__ __forceinline__ float inverse_root(float v) {
-  const bool small = v < 0x1p-126f;
-  const float r = __builtin_amdgcn_rsqf(small ? v * 0x1p64f : v);
-  return small ? r * 0x1p32f : r;
-}
-
 template <bool ODD, int CH>
 __device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Place (&at)[CH], const spqr_residual_norm_t& p, const void* weight, const void* bias,
                                           const Raw (&w)[CH], const Raw (&b)[CH], RowSum& sum) {
@@ -138,7 +130,7 @@ __device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Pla
 #pragma unroll
       for (int e = 0; e < 8; ++e) v[c][e] -= mean;
   }
-  const float r = inverse_root(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
+  const float r = __builtin_amdgcn_rsqf(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
 #pragma unroll
   for (int c = 0; c < CH; ++c) {
     float x[8], y[8];
@@ -277,7 +269,7 @@ static void launch_rows_any(const spqr_residual_norm_t& p, int lanes, int thread
 }
 
 // ---------------------------------------------------------------------------------------------------------------------
-// Longer rows, and rows of fewer than eight elements.
+// Longer rows, rows of fewer than eight elements, and an eps below 2^-126.
 // ---------------------------------------------------------------------------------------------------------------------
 template <int CH>
 __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at)[CH], int n, float eps, int weight_dtype, float offset,
@@ -418,7 +410,9 @@ extern "C" int spqr_residual_norm(const spqr_residual_norm_t* p, void* stream) {
   const int64_t grid = ((int64_t)p->rows + per - 1) / per;
   const hipStream_t st = static_cast<hipStream_t>(stream);
   const int ch = (runs + lanes - 1) / lanes;
-  if (ch <= 1 && p->width >= 8) {
+  // (The card's inverse root takes subnormal numbers for 0: with an eps that keeps nothing from being one, the other kernel's division and root.  A
+  // case of it beside the inverse root cost 4096 gated rows 1 to 3 us.)
+  if (ch <= 1 && p->width >= 8 && p->eps >= 0x1p-126f) {
     if ((!p->x && !p->sum) || p->x_dtype == SPQR_F32) launch_rows_any<float>(*p, lanes, threads, grid, st);
     else if (p->x_dtype == SPQR_F16) launch_rows_any<_Float16>(*p, lanes, threads, grid, st);
     else launch_rows_any<__bf16>(*p, lanes, threads, grid, st);
