@@ -90,66 +90,51 @@ __device__ __forceinline__ void floats_at(const Raw& r, int dtype, const Place& 
     for (int e = 0; e + d < 8; ++e) v[e] = at.shift & d ? v[e + d] : v[e];
 }
 // What is no element counts nothing.
-template <bool ODD, int CH>
-__device__ __forceinline__ float sum_of(const float (&v)[CH][8], const Place (&at)[CH]) {
-  float sum = 0.f;
+template <bool ODD>
+__device__ __forceinline__ float sum_of(const float (&v)[8], const Place& at) {
+  float s = 0.f;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) s += !ODD || e < at[c].count ? v[c][e] : 0.f;
-    sum += ODD || at[c].count > 0 ? s : 0.f;
-  }
-  return sum;
+  for (int e = 0; e < 8; ++e) s += !ODD || e < at.count ? v[e] : 0.f;
+  return ODD || at.count > 0 ? s : 0.f;
 }
-template <bool ODD, int CH>
-__device__ __forceinline__ float squares_of(const float (&v)[CH][8], const Place (&at)[CH]) {
-  float sum = 0.f;
+template <bool ODD>
+__device__ __forceinline__ float squares_of(const float (&v)[8], const Place& at) {
+  float s = 0.f;
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    float s = 0.f;
-#pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      const float x = !ODD || e < at[c].count ? v[c][e] : 0.f;
-      s = fmaf(x, x, s);
-    }
-    sum += ODD || at[c].count > 0 ? s : 0.f;
+  for (int e = 0; e < 8; ++e) {
+    const float x = !ODD || e < at.count ? v[e] : 0.f;
+    s = fmaf(x, x, s);
   }
-  return sum;
+  return ODD || at.count > 0 ? s : 0.f;
 }
 
-template <bool ODD, int CH>
-__device__ __forceinline__ void norm_rows(int kind, float (&v)[CH][8], const Place (&at)[CH], const spqr_residual_norm_t& p, const void* weight, const void* bias,
-                                          const Raw (&w)[CH], const Raw (&b)[CH], RowSum& sum) {
+template <bool ODD>
+__device__ __forceinline__ void norm_rows(int kind, float (&v)[8], const Place& at, const spqr_residual_norm_t& p, const void* weight, const void* bias, const Raw& w,
+                                          const Raw& b, RowSum& sum) {
   if (kind == SPQR_NORM_NONE) return;
   const float inverse = 1.f / (float)p.width;
   if (kind == SPQR_NORM_LAYER) {
     const float mean = sum(sum_of<ODD>(v, at)) * inverse;
 #pragma unroll
-    for (int c = 0; c < CH; ++c)
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[c][e] -= mean;
+    for (int e = 0; e < 8; ++e) v[e] -= mean;
   }
   const float r = __builtin_amdgcn_rsqf(fmaf(sum(squares_of<ODD>(v, at)), inverse, p.eps));
+  float x[8];
+  if (weight) {
+    floats_at<ODD>(w, p.weight_dtype, at, x);
+    if (p.weight_offset != 0.f)
 #pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    float x[8], y[8];
-    if (weight) {
-      floats_at<ODD>(w[c], p.weight_dtype, at[c], x);
-      if (p.weight_offset != 0.f)
+      for (int e = 0; e < 8; ++e) x[e] += p.weight_offset;
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] += p.weight_offset;
+    for (int e = 0; e < 8; ++e) v[e] *= r * x[e];
+  } else {
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[c][e] *= r * x[e];
-    } else {
+    for (int e = 0; e < 8; ++e) v[e] *= r;
+  }
+  if (bias) {
+    floats_at<ODD>(b, p.weight_dtype, at, x);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) v[c][e] *= r;
-    }
-    if (bias) {
-      floats_at<ODD>(b[c], p.weight_dtype, at[c], y);
-#pragma unroll
-      for (int e = 0; e < 8; ++e) v[c][e] += y[e];
-    }
+    for (int e = 0; e < 8; ++e) v[e] += x[e];
   }
 }
 
@@ -159,88 +144,68 @@ template <> struct TypeOf<__bf16> { static constexpr int value = SPQR_BF16; };
 
 // `lanes` threads a row.  MANY: rows in turn; the next row's terms are on their way while one is worked out (4096 gated rows of 6656: 119 us with a
 // workgroup a row).
-template <typename X, typename Y, bool ODD, bool MANY, int CH = 1>
-__global__ void __launch_bounds__(1024 / CH) norm_rows_kernel(spqr_residual_norm_t p, int lanes) {
+template <typename X, typename Y, bool ODD, bool MANY>
+__global__ void __launch_bounds__(1024) norm_rows_kernel(spqr_residual_norm_t p, int lanes) {
   __shared__ __align__(16) float part[2][16];
   constexpr int XT = TypeOf<X>::value, YT = TypeOf<Y>::value;
   const int n = p.width, in_row = threadIdx.x & (lanes - 1), per = blockDim.x / lanes, mine = threadIdx.x / lanes;
   const bool has_x = p.x != nullptr, has_y = p.y != nullptr, has_gate = p.gate != nullptr;
-  Place at[CH];
-#pragma unroll
-  for (int c = 0; c < CH; ++c) {
-    at[c].col = 8 * (in_row + lanes * c);
-    at[c].count = min(max(n - at[c].col, 0), 8);
-    at[c].from = min(at[c].col, n - 8);
-    at[c].shift = at[c].count > 0 ? at[c].col - at[c].from : 0;
-  }
+  Place at;
+  at.col = 8 * in_row;
+  at.count = min(max(n - at.col, 0), 8);
+  at.from = min(at.col, n - 8);
+  at.shift = at.count > 0 ? at.col - at.from : 0;
   RowSum sum{part, lanes, 0};
   int64_t first = (int64_t)blockIdx.x * per, t = min(first + mine, (int64_t)p.rows - 1);
-  Raw y[CH], x[CH], g[CH];
+  Raw y, x, g;
   auto load_row = [&](int64_t t, bool gate) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if (has_y) load(y[c], YT, p.y, t * p.y_stride + at[c].from);
-      if (has_x) load(x[c], XT, p.x, t * p.x_stride + at[c].from);
-      if (gate) load(g[c], p.gate_dtype, p.gate, t * p.gate_stride + at[c].from);
-    }
+    if (has_y) load(y, YT, p.y, t * p.y_stride + at.from);
+    if (has_x) load(x, XT, p.x, t * p.x_stride + at.from);
+    if (gate) load(g, p.gate_dtype, p.gate, t * p.gate_stride + at.from);
   };
-  auto load_vectors = [&](Raw (&w)[CH], Raw (&b)[CH], const void* weight, const void* bias) {
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if (weight) load(w[c], p.weight_dtype, weight, at[c].from);
-      if (bias) load(b[c], p.weight_dtype, bias, at[c].from);
-    }
+  auto load_vectors = [&](Raw& w, Raw& b, const void* weight, const void* bias) {
+    if (weight) load(w, p.weight_dtype, weight, at.from);
+    if (bias) load(b, p.weight_dtype, bias, at.from);
   };
   load_row(t, has_gate);
   for (; first < p.rows; first += (int64_t)gridDim.x * per) {
     const bool live = first + mine < p.rows;     // (other threads take part in the sums, and store nothing)
     const int64_t here = t;
-    float v[CH][8], xs[CH][8], f[CH][8];
-    Raw w[CH], b[CH];
+    float v[8], xs[8], f[8];
+    Raw w, b;
     load_vectors(w, b, p.y_weight, p.y_bias);
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if (has_y) floats_at<ODD>(y[c], YT, at[c], v[c]);
-      if (has_x) floats_at<ODD>(x[c], XT, at[c], xs[c]);
-      if (has_gate) floats_at<ODD>(g[c], p.gate_dtype, at[c], f[c]);
-    }
+    if (has_y) floats_at<ODD>(y, YT, at, v);
+    if (has_x) floats_at<ODD>(x, XT, at, xs);
+    if (has_gate) floats_at<ODD>(g, p.gate_dtype, at, f);
     const int64_t next = first + (int64_t)gridDim.x * per;
     if (MANY && next < p.rows) {
       t = min(next + mine, (int64_t)p.rows - 1);
-      load_row(t, has_gate && p.gate_stride != 0);
+      load_row(t, has_gate && p.gate_stride != 0);         // (one gate for all rows stays in its registers)
     }
     if (has_y) {
       norm_rows<ODD>(p.norm_y, v, at, p, p.y_weight, p.y_bias, w, b, sum);
+      if (has_gate) {
+        if (p.act == SPQR_ACT_SIGMOID) {
 #pragma unroll
-      for (int c = 0; c < CH; ++c) {
-        if (has_gate) {
-          if (p.act == SPQR_ACT_SIGMOID) {
+          for (int e = 0; e < 8; ++e) f[e] = activated(SPQR_ACT_SIGMOID, f[e]);
+        } else if (p.act != SPQR_ACT_NONE) {
 #pragma unroll
-            for (int e = 0; e < 8; ++e) f[c][e] = activated(SPQR_ACT_SIGMOID, f[c][e]);
-          } else if (p.act != SPQR_ACT_NONE) {
-#pragma unroll
-            for (int e = 0; e < 8; ++e) f[c][e] = activated(p.act, f[c][e]);
-          }
-#pragma unroll
-          for (int e = 0; e < 8; ++e) v[c][e] *= f[c][e];
+          for (int e = 0; e < 8; ++e) f[e] = activated(p.act, f[e]);
         }
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] *= p.scale;
+        for (int e = 0; e < 8; ++e) v[e] *= f[e];
       }
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] *= p.scale;
     }
     load_vectors(w, b, p.x_weight, p.x_bias);
+    if (has_x)
 #pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if (has_x)
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[c][e] = has_y ? fmaf(p.skip, xs[c][e], v[c][e]) : p.skip * xs[c][e];
-      if (p.sum && live && at[c].count > 0) store_row8_as(XT, p.sum, here * p.sum_stride, at[c].col, n, v[c]);
-    }
+      for (int e = 0; e < 8; ++e) v[e] = has_y ? fmaf(p.skip, xs[e], v[e]) : p.skip * xs[e];
+    if (p.sum && live && at.count > 0) store_row8_as(XT, p.sum, here * p.sum_stride, at.col, n, v);
     if (p.out) {
       norm_rows<ODD>(p.norm_x, v, at, p, p.x_weight, p.x_bias, w, b, sum);
-#pragma unroll
-      for (int c = 0; c < CH; ++c)
-        if (live && at[c].count > 0) store_row8_as(p.out_dtype, p.out, here * p.out_stride, at[c].col, n, v[c]);
+      if (live && at.count > 0) store_row8_as(p.out_dtype, p.out, here * p.out_stride, at.col, n, v);
     }
     if (!MANY) return;
   }
