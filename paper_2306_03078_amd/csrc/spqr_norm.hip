@@ -211,13 +211,14 @@ __global__ void __launch_bounds__(1024) norm_rows_kernel(spqr_residual_norm_t p,
   }
 }
 
-constexpr int64_t kThreads = 512 * 1024;         // as many as run at once
+// Threads that run at once: of the kernel with a row a workgroup (59 to 67 registers), of the one with rows in turn (97 to 126; as many as of the
+// other are two sets of workgroups, the second without a row on its way: 4096 rows of 6656 83 us in place of 81, 1030 of 8192 25 in place of 23.6).
+constexpr int64_t kThreads = 512 * 1024, kThreadsInTurn = 256 * 1024;
 
 template <typename X, typename Y, bool ODD>
 static void launch_rows(const spqr_residual_norm_t& p, int lanes, int threads, int64_t groups, hipStream_t st) {
-  const int64_t most = kThreads / threads;
-  if (groups <= most) hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, false>), dim3((unsigned)groups), dim3(threads), 0, st, p, lanes);
-  else hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, true>), dim3((unsigned)most), dim3(threads), 0, st, p, lanes);
+  if (groups <= kThreads / threads) hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, false>), dim3((unsigned)groups), dim3(threads), 0, st, p, lanes);
+  else hipLaunchKernelGGL((norm_rows_kernel<X, Y, ODD, true>), dim3((unsigned)(kThreadsInTurn / threads)), dim3(threads), 0, st, p, lanes);
 }
 
 template <typename X, bool ODD>
@@ -275,7 +276,8 @@ __device__ __forceinline__ void norm(int kind, float (&v)[CH][8], const int (&at
   }
 }
 
-// `lanes` threads a row, CH runs of eight elements each, which stay in registers from the loads to the stores.  first: of the launch's workgroups.
+// `lanes` threads a row, CH runs of eight elements each, kept from the loads to the stores: in registers up to four runs (32768 elements), a good
+// part of eight in memory (760 bytes a lane).  first: of the launch's workgroups.
 template <int CH>
 __global__ void __launch_bounds__(1024) residual_norm_kernel(spqr_residual_norm_t p, int lanes, int64_t first) {
   __shared__ __align__(16) float part[2][16];
