@@ -14,8 +14,9 @@ constexpr int kTile = SPQR_ADAPTER_TILE;
 //
 // A workgroup a slot (the last one: rows of no adapter).  Each counts the rows of all slots for itself, which gives the tiles before
 // its own; a wavefront has an equal part of the requests, in order, counts those of the slot, and writes their rows behind those of the wavefronts
-// before it.  Trips to memory and to LDS one after the other bound it: 4096 rows of 200 slots 6.2 us (256 threads, a barrier for every 256
-// requests: 15.7), 64 requests of 48 slots 4.5 us.
+// before it.  Trips to memory and to LDS one after the other bound it: 4096 rows of 200 slots 6.0 us (256 threads, a barrier for every 256
+// requests: 15.7), 64 requests of 48 slots 4.6 us; with many rows of many slots what every workgroup reads: 65536 rows of 4096 slots 316 us, 2^20 rows
+// of 200 slots 650 us, of 4096 slots 6.4 ms.
 constexpr int kPlanAhead = 4;
 
 template <bool BY_ROW, int WAVES>
@@ -442,7 +443,7 @@ template <> struct Parts<__bf16> { static constexpr int N = 3; };
 // out[row][m] = y[row][m] + factor[row] * sum_k B[m][k] v[row][k] for the m of [m0, m1) and up to 64 rows, 32 * H ranks (H = 0: 16).  The parts of v
 // lie in LDS as operands, NS * 16 rows of them.  A wavefront takes 64 m at a time, four products side by side, whose results are 4 neighbouring m
 // of 4 rows in every lane; the workgroup's four are neighbours, so that a row is read and written 1 KB at a time (wavefronts with rows of
-// their own and 256 bytes of each: 168 us in place of 150 for 5000 rows of 8192 + 1024 + 1024 m, 64 ranks, binary32).  The next weights and elements of y are on their way meanwhile.
+// their own and 256 bytes of each: 168 us in place of 150 for 5000 rows of 8192 + 1024 + 1024 m, 64 ranks, binary32, before the split below).  The next weights and elements of y are on their way meanwhile.
 // Ranks that a bank does not have (three times 32 of four) read its last ones and meet zeros.
 template <typename T, typename Y, int H, int NS>
 __device__ __forceinline__ void expand_rows(const Call& c, const Projection& p, const Tile& t, int tile, int sub0, int rank, int m0, int m1, f32x4* sums,
@@ -709,7 +710,7 @@ __device__ __forceinline__ void copy_rows(const Projection& p, const Tile& t, in
 }
 
 // The outputs' rows lie in a line, tile after tile, projection after projection, 256 elements a piece; a workgroup takes an equal part of it, as long as
-// no projection of a tile ends.  (A grid of pieces of 1024, whose last ones leave half of the card idle: 150 us in place of 103 for those 5000 rows.)
+// no projection of a tile ends.  (A grid of pieces of 1024, whose last ones leave half of the card idle: 150 us in place of 103 for those 5000 rows, which take 98 to 100 now.)
 // KIND: steps of up to 16 rows (registers for twice the workgroups), any rows, ranks above 64.
 enum Kind { kFew, kAny, kLong };
 template <typename T, typename Y, Kind KIND>

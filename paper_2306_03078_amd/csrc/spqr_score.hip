@@ -260,7 +260,8 @@ __global__ void __launch_bounds__(NT) score_kernel(spqr_token_logprobs_t p, int 
   if (k > 0) {
     int count = found;
     if (count > kCandidates) {
-      // Many equal logits around the bound: one after the other, each the best below the last.
+      // Many equal logits around the bound (all of a row alike; masks by the type's lowest value that leave fewer than k): one after the other, each the
+      // best below the last, the row read again for each.  2048 rows of 65537 with 10 alternatives 663 us in place of 61, one row of 32000 28 in place of 10.
       uint64_t last = ~0ull;
       for (count = 0; count < k; ++count) {
         uint64_t b = 0;
