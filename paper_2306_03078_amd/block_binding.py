@@ -75,21 +75,26 @@ def _lib():
     return lib
 
 
-def _run(name, index, desc, *args):
-    """One of the entries, on the handle's device: launches go to the current one, on its current stream."""
+def _run(name, index, stream, desc, *args):
+    """One of the entries, on the handle's device: launches go to the current one, on its current stream where none is given."""
     if S._current_device() != index:
         import torch
         with torch.cuda.device(index):
-            return _run(name, index, desc, *args)
-    rc = B._call(_entry[name], desc, *args, S._raw_stream(index))
+            return _run(name, index, stream, desc, *args)
+    rc = B._call(_entry[name], desc, *args, S._raw_stream(index) if stream is None else _address(stream, index))
     if rc != 0:
         raise SpQRError(int(rc), name)
 
 
-def _on(stream, index):
-    """A call's stream as the current one, for what the call makes (binding._on); of the handle's device."""
+def _address(stream, index):
     if stream.device_index != index:
         raise ValueError(f"a stream of cuda:{stream.device_index} for a handle on cuda:{index}")
+    return stream.cuda_stream
+
+
+def _on(stream, index):
+    """A call's stream as the current one, for what the call makes (binding._on); of the handle's device."""
+    _address(stream, index)
     return B._on(stream)
 
 
@@ -154,7 +159,7 @@ def spqr_residual_norm(norm: SpQRResidualNorm, x=None, y=None, gate=None, *, sum
     made where there are both x and y, or written to `sum` (which may be x); else None.  The norm, of the handle's out_dtype, is made or
     written to `out`; None with out_dtype None."""
     index, dtypes = norm._index, S._dtypes
-    if stream is not None:
+    if stream is not None and ((sum is None and x is not None and y is not None) or (out is None and norm.out_dtype is not None)):
         with _on(stream, index):
             return spqr_residual_norm(norm, x, y, gate, sum=sum, out=out)
     rows = y if x is None else x
@@ -197,7 +202,7 @@ def spqr_residual_norm(norm: SpQRResidualNorm, x=None, y=None, gate=None, *, sum
     d = norm.desc
     _norm_types.pack_into(d, 0, count, width, x_type, y_type, gate_type, norm._out_type)
     _norm_rows.pack_into(d, _norm_rows_at, x_at, y_at, gate_at, sum_at, out_at, x_stride, y_stride, sum_stride, out_stride, gate_stride)
-    _run("spqr_residual_norm", index, d)
+    _run("spqr_residual_norm", index, stream, d)
     return sum, out
 
 
@@ -227,14 +232,11 @@ def spqr_adapter_plan(plan: SpQRAdapterPlan, adapter, q_start=None, stream=None)
     """The step's rows by adapter.  adapter: int32 [requests], the slot of each request (anything outside: none), with q_start int32
     [requests + 1] (SpQRStep.q_start); or [rows], without."""
     d, index = plan.desc, plan._index
-    if stream is not None:
-        with _on(stream, index):
-            return spqr_adapter_plan(plan, adapter, q_start)
     for name, a, n in (("adapter", adapter, plan.rows if q_start is None else adapter.numel()), ("q_start", q_start, adapter.numel() + 1)):
         if a is not None and (a.dtype != S._int32 or not a.is_contiguous() or a.dim() != 1 or a.numel() != n or a.get_device() != index):
             raise ValueError(f"{name}: a contiguous int32 tensor [{n}] on {plan.device}, not {a.dtype} {list(a.shape)} on {a.device}")
     d.requests, d.adapter, d.q_start = adapter.numel(), adapter.data_ptr(), None if q_start is None else q_start.data_ptr()
-    _run("spqr_adapter_plan", index, d)
+    _run("spqr_adapter_plan", index, stream, d)
     return plan
 
 
@@ -327,9 +329,9 @@ def spqr_adapters(bank: SpQRAdapters, plan: SpQRAdapterPlan, x, ys=None, outs=No
     [rows, m[p]] of one type.  ys None: zeros (outs are float32 unless given).  outs None: new tensors; outs may be ys.  Rows that the
     plan has in no tile are left as they are."""
     d, index, dtypes = bank.desc, bank._index, S._dtypes
-    if stream is not None:
+    if stream is not None and outs is None:
         with _on(stream, index):
-            return spqr_adapters(bank, plan, x, ys, outs)
+            return spqr_adapters(bank, plan, x, ys)
     rows, k, ms = plan.rows, len(bank.m), bank.m
     if plan._index != index:
         raise ValueError(f"a plan on {plan.device}, banks on {bank.device}")
@@ -356,7 +358,7 @@ def spqr_adapters(bank: SpQRAdapters, plan: SpQRAdapterPlan, x, ys=None, outs=No
         fields[SPQR_MAX_FUSED + p] = outs[p].data_ptr()
     _bank_rows.pack_into(d, _bank_rows_at, *fields)
     d.y_dtype = dtypes[dtype]
-    _run("spqr_adapters", index, d, plan._at)
+    _run("spqr_adapters", index, stream, d, plan._at)
     return outs
 
 
@@ -387,9 +389,6 @@ def spqr_token_logprobs(scores: SpQRScores, logits, tokens=None, scale: float = 
     """Fills `scores` for logits [rows, vocab] (float32, float16, bfloat16): log softmax(scale * logits) of tokens int32 [rows, given]
     ([rows] where given is 1), entropies, the most probable tokens.  Fewer rows than the handle's: the first ones are filled."""
     d, index = scores.desc, scores._index
-    if stream is not None:
-        with _on(stream, index):
-            return spqr_token_logprobs(scores, logits, tokens, scale)
     if logits.dim() != 2 or logits.shape[0] > scores.rows:
         raise ValueError(f"logits: up to {scores.rows} rows of {scores.vocab}, not {list(logits.shape)}")
     rows = logits.shape[0]
@@ -402,5 +401,5 @@ def spqr_token_logprobs(scores: SpQRScores, logits, tokens=None, scale: float = 
     elif tokens is not None:
         raise ValueError("tokens: this handle has given = 0")
     d.scale = scale
-    _run("spqr_token_logprobs", index, d)
+    _run("spqr_token_logprobs", index, stream, d)
     return scores

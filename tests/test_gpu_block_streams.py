@@ -99,3 +99,20 @@ def test_a_stream_of_the_call_in_a_capture():
         want = K.spqr_residual_norm(norm, x, y)
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_the_current_stream_is_the_one_it_was():
+    """After calls with stream=, ones that are refused too, on the default stream and inside another stream's context."""
+    norm = K.SpQRResidualNorm(WIDTH)
+    x, side, other = torch.randn(ROWS, WIDTH, device="cuda"), torch.cuda.Stream(), torch.cuda.Stream()
+    want = K.spqr_residual_norm(norm, x, x)
+    torch.cuda.synchronize()
+    for context in (torch.cuda.default_stream(), other):
+        with torch.cuda.stream(context):
+            got = K.spqr_residual_norm(norm, x, x, stream=side)
+            assert torch.cuda.current_stream() == context
+            with pytest.raises(ValueError):
+                K.spqr_residual_norm(norm, x, x[:3], stream=side)
+            assert torch.cuda.current_stream() == context
+        side.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(got, want))

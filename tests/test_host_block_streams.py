@@ -74,7 +74,7 @@ def world(monkeypatch):
     monkeypatch.setattr(B, "_call", call)
     monkeypatch.setattr(S, "_raw_stream", lambda index: current[0].cuda_stream)
     monkeypatch.setattr(S, "_current_device", lambda: 0)
-    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(B, "_on", On)
     monkeypatch.setattr(K, "_empty", lambda shape, dtype, device: Tensor(shape, dtype, current[0]))
     monkeypatch.setattr(K, "_empty_like", lambda t: Tensor(t.shape, t.dtype, current[0]))
     return got, (lambda: current[0]), One()

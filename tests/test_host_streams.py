@@ -46,13 +46,14 @@ def world(monkeypatch):
     monkeypatch.setattr(B, "_call", lambda entry, desc, *args: launched.append(args[-1]) or 0)
     for m in (B, E):
         monkeypatch.setattr(m, "load_library", Lib)
+    monkeypatch.setattr(E, "_on", On)
     monkeypatch.setattr(E, "_lib", Lib)
     address = lambda stream: (current[0] if stream is None else stream).cuda_stream  # noqa: E731
     monkeypatch.setattr(B, "_stream_ptr", address)
     monkeypatch.setattr(E, "_stream_ptr", address)
     monkeypatch.setattr(S, "_raw_stream", lambda index: current[0].cuda_stream)
     monkeypatch.setattr(S, "_current_device", lambda: 0)
-    monkeypatch.setattr(torch.cuda, "stream", On)
+    monkeypatch.setattr(B, "_on", On)
     monkeypatch.setattr(torch.cuda, "current_stream", lambda *_: current[0])
     monkeypatch.setattr(torch, "empty", noting(torch.empty))
     monkeypatch.setattr(torch, "empty_like", noting(lambda t, **_: t))
